@@ -187,6 +187,7 @@ def _hold(case, s):
     if "tokens" in s:
         vocab, top = case.get("vocab") or case["cout"], case["top"]
         s.update(logprob=new(rows, case["given"], dtype=f32), lse=new(rows, dtype=f32), entropy=new(rows, dtype=f32),
+                 shift=new(rows, 2, dtype=f32) if kind == "logp_train" else None,
                  top_index=new(rows, top, dtype=torch.int32) if top else None, top_logprob=new(rows, top, dtype=f32) if top else None,
                  lp_scratch=scratch(xnor.logprobs_workspace_bytes(rows, vocab, top)))
         if kind == "logp_train":
@@ -286,8 +287,8 @@ def _plain(s):
 # ---- the framework's calls ------------------------------------------------------------------------------------------
 def _own_logp(xnor, s, logits, rows, vocab):
     case = s["case"]
-    xnor.xnor_logprobs(logits, s["tokens"], s["logprob"], s["lse"], s["entropy"], s["top_index"], s["top_logprob"], s["lp_scratch"], rows,
-                       vocab, case["given"], case["top"])
+    xnor.xnor_logprobs(logits, s["tokens"], s["logprob"], s["lse"], s["shift"], s["entropy"], s["top_index"], s["top_logprob"], s["lp_scratch"],
+                       rows, vocab, case["given"], case["top"])
     r = {"logprob": s["logprob"], "lse": s["lse"], "entropy": s["entropy"]}
     return dict(r, top_index=s["top_index"], top_logprob=s["top_logprob"]) if case["top"] else r
 
@@ -302,7 +303,7 @@ def _own(s):
     if kind in ("logp", "logp_train"):
         r = _own_logp(xnor, s, s["logits"], rows, case["vocab"])
         if kind == "logp_train":
-            xnor.xnor_logprobs_backward(s["logits"], s["tokens"], s["lse"], s["entropy"], s["g_logprob"], s["g_entropy"], s["g_logits"], rows,
+            xnor.xnor_logprobs_backward(s["logits"], s["tokens"], s["shift"], s["entropy"], s["g_logprob"], s["g_entropy"], s["g_logits"], rows,
                                         case["vocab"], case["given"])
             r["g_logits"] = s["g_logits"]
         return r
