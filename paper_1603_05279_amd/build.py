@@ -46,8 +46,9 @@ def build_binding(incremental: bool = False) -> str:
     """The host-only extension module that marshals tensors for libxnor's entry points (torch's own headers and libraries)."""
     import sysconfig
     import torch
-    src, header = os.path.join(CSRC, "binding.cpp"), os.path.join(ROOT, "include", "xnor.h")
-    if incremental and os.path.exists(BINDING) and os.path.getmtime(BINDING) >= max(map(os.path.getmtime, (src, header))):
+    src = os.path.join(CSRC, "binding.cpp")
+    headers = [os.path.join(ROOT, "include", h) for h in ("xnor.h", "xnor_lowbit.h")]
+    if incremental and os.path.exists(BINDING) and os.path.getmtime(BINDING) >= max(map(os.path.getmtime, [src] + headers)):
         return BINDING
     home = os.path.dirname(torch.__file__)
     inc = [os.path.join(ROOT, "include"), sysconfig.get_paths()["include"], os.path.join(home, "include"),

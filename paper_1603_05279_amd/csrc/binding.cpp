@@ -11,6 +11,7 @@
 #include <dlfcn.h>
 
 #include "xnor.h"
+#include "xnor_lowbit.h"
 
 namespace {
 
@@ -51,6 +52,80 @@ int num(PyObject *o)
     if (v == (unsigned long)-1 && PyErr_Occurred()) throw PythonError{};
     return (int)v;
 }
+int64_t area(PyObject *n, PyObject *m) { return (int64_t)num(n) * num(m); }
+
+double real(PyObject *o)
+{
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw PythonError{};
+    return v;
+}
+
+// Arguments of the calls of xnor_lowbit.h.  Their tensors are looked at more closely, since a row too few is a read out of range: each has to
+// hold what the sizes say.
+c10::ScalarType scalar_type(int type)
+{
+    return type == XNOR_F32 ? c10::ScalarType::Float : type == XNOR_BF16 ? c10::ScalarType::BFloat16 : c10::ScalarType::Half;
+}
+// the xnor_dtype of a real tensor
+int dtype(PyObject *o)
+{
+    if (!THPVariable_Check(o)) fail(PyExc_TypeError, "expected a tensor");
+    switch (THPVariable_Unpack(o).scalar_type()) {
+    case c10::ScalarType::Float: return XNOR_F32;
+    case c10::ScalarType::BFloat16: return XNOR_BF16;
+    case c10::ScalarType::Half: return XNOR_F16;
+    default: fail(PyExc_ValueError, "expected float32, bfloat16 or float16");
+    }
+}
+int token_bytes(PyObject *o)
+{
+    if (o == Py_None) return 4;
+    if (!THPVariable_Check(o)) fail(PyExc_TypeError, "expected a tensor or None");
+    switch (THPVariable_Unpack(o).scalar_type()) {
+    case c10::ScalarType::Int: return 4;
+    case c10::ScalarType::Long: return 8;
+    default: fail(PyExc_ValueError, "expected int32 or int64 tokens");
+    }
+}
+void *dense(PyObject *o, c10::ScalarType type, int64_t count)
+{
+    void *p = tensor(o, type);
+    if (o != Py_None && THPVariable_Unpack(o).numel() < count) fail(PyExc_ValueError, "a tensor holds less than the sizes say");
+    return p;
+}
+float *dense_f32(PyObject *o, int64_t count) { return static_cast<float *>(dense(o, c10::ScalarType::Float, count)); }
+void *tokens(PyObject *o, int64_t count) { return dense(o, token_bytes(o) == 8 ? c10::ScalarType::Long : c10::ScalarType::Int, count); }
+template <class T> T *dense_of(PyObject *o, c10::ScalarType type, int64_t count) { return static_cast<T *>(dense(o, type, count)); }
+
+// Rows of `cols` neighbours: a matrix whose rows may lie apart, or any dense tensor of that many elements.
+bool lie_apart(const at::Tensor &t, int64_t rows, int64_t cols)
+{
+    return t.dim() == 2 && t.size(0) == rows && t.size(1) == cols && rows > 1 && t.stride(0) > cols && (cols == 1 || t.stride(1) == 1);
+}
+void *rows(PyObject *o, int type, int64_t n, int64_t cols)
+{
+    if (o == Py_None) return nullptr;
+    if (!THPVariable_Check(o)) fail(PyExc_TypeError, "expected a tensor or None");
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (t.is_cuda() && t.scalar_type() == scalar_type(type) && lie_apart(t, n, cols)) return t.data_ptr();
+    return dense(o, scalar_type(type), n * cols);
+}
+int64_t stride(PyObject *o, int64_t n, int64_t cols)
+{
+    if (o == Py_None) return cols;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    return lie_apart(t, n, cols) ? t.stride(0) : cols;
+}
+int64_t groups(int64_t cols, int64_t group) { return group > 0 ? (cols + group - 1) / group : 1; }
+
+// Sizes that the library states, for the checks of images and workspaces.
+#define XNOR_QUERIES(X)                                                                               \
+    X(xnor_rmsnorm_backward_workspace_bytes) X(xnor_w4_wimg_bytes) X(xnor_w4_linear_workspace_bytes) \
+    X(xnor_logprobs_workspace_bytes)
+#define XNOR_QUERY_POINTER(NAME) decltype(&::NAME) p_##NAME = nullptr;
+XNOR_QUERIES(XNOR_QUERY_POINTER)
+void *bytes(PyObject *o, size_t count) { return dense(o, c10::ScalarType::Byte, (int64_t)count); }
 
 // A descriptor (xnor.py's ctypes structure, nothing else that holds as many bytes) through the buffer protocol; held for the
 // duration of the call.
@@ -120,7 +195,49 @@ void *stream(PyObject *o)
     X(xnor_conv2d_binactiv, 15, u32(a[0]), u32(a[1]), u8(a[2]), f32(a[3]), f32(a[4]), f32(a[5]), f32(a[6]), f32(a[7]),    \
       u32(a[8]), f32(a[9]), f32(a[10]), u8(a[11]), Desc(a[12]), num(a[13]))                                               \
     X(xnor_conv2d_binactiv_noalloc, 14, u32(a[0]), u32(a[1]), u8(a[2]), f32(a[3]), f32(a[4]), f32(a[5]), f32(a[6]),       \
-      f32(a[7]), u32(a[8]), f32(a[9]), f32(a[10]), Desc(a[11]), num(a[12]))
+      f32(a[7]), u32(a[8]), f32(a[9]), f32(a[10]), Desc(a[11]), num(a[12]))                                               \
+    X(xnor_rmsnorm_q8, 13, rows(a[0], dtype(a[0]), num(a[8]), num(a[9])), stride(a[0], num(a[8]), num(a[9])),             \
+      rows(a[1], dtype(a[0]), num(a[8]), num(a[9])), stride(a[1], num(a[8]), num(a[9])), dense_f32(a[2], num(a[9])),      \
+      dense(a[3], scalar_type(dtype(a[0])), area(a[8], a[9])),                                                            \
+      dense_of<int8_t>(a[4], c10::ScalarType::Char, area(a[8], a[9])),                                                    \
+      dense_f32(a[5], num(a[8]) * groups(num(a[9]), num(a[10]))), dense(a[6], scalar_type(dtype(a[0])), area(a[8], a[9])),\
+      dense_f32(a[7], num(a[8])), num(a[8]), num(a[9]), num(a[10]), dtype(a[0]), (float)real(a[11]))                      \
+    X(xnor_rmsnorm_backward, 11, rows(a[0], dtype(a[0]), num(a[8]), num(a[9])), stride(a[0], num(a[8]), num(a[9])),       \
+      dense_f32(a[1], num(a[8])), dense_f32(a[2], num(a[9])), rows(a[3], dtype(a[0]), num(a[8]), num(a[9])),              \
+      stride(a[3], num(a[8]), num(a[9])), rows(a[4], dtype(a[0]), num(a[8]), num(a[9])),                                  \
+      stride(a[4], num(a[8]), num(a[9])), dense(a[5], scalar_type(dtype(a[0])), area(a[8], a[9])),                        \
+      dense_f32(a[6], num(a[9])), bytes(a[7], p_xnor_rmsnorm_backward_workspace_bytes(num(a[8]), num(a[9]))), num(a[8]),  \
+      num(a[9]), dtype(a[0]))                                                                                             \
+    X(xnor_w4_quantize, 8, rows(a[0], dtype(a[0]), num(a[4]), num(a[5])), stride(a[0], num(a[4]), num(a[5])),             \
+      dense_of<uint8_t>(a[1], c10::ScalarType::Byte, num(a[4]) * groups(num(a[5]), 32) * 16),                             \
+      dense_f32(a[2], num(a[4]) * groups(num(a[5]), num(a[6]))),                                                          \
+      dense_of<uint8_t>(a[3], c10::ScalarType::Byte, num(a[4]) * groups(num(a[5]), num(a[6]))), num(a[4]), num(a[5]),     \
+      num(a[6]), dtype(a[0]))                                                                                             \
+    X(xnor_w4_pack, 8, dense_of<uint8_t>(a[0], c10::ScalarType::Byte, num(a[4]) * groups(num(a[5]), 32) * 16),            \
+      dense_f32(a[1], num(a[4]) * groups(num(a[5]), num(a[6]))),                                                          \
+      dense_of<uint8_t>(a[2], c10::ScalarType::Byte, num(a[4]) * groups(num(a[5]), num(a[6]))),                           \
+      bytes(a[3], p_xnor_w4_wimg_bytes(num(a[4]), num(a[5]), num(a[6]))), num(a[4]), num(a[5]), num(a[6]))                \
+    X(xnor_w4_linear, 9, rows(a[0], dtype(a[0]), num(a[4]), num(a[5])), stride(a[0], num(a[4]), num(a[5])),               \
+      bytes(a[1], p_xnor_w4_wimg_bytes(num(a[6]), num(a[5]), num(a[7]))),                                                 \
+      dense(a[2], scalar_type(dtype(a[0])), area(a[4], a[6])),                                                            \
+      bytes(a[3], p_xnor_w4_linear_workspace_bytes(num(a[4]), num(a[5]), num(a[6]), num(a[7]))), num(a[4]), num(a[5]),    \
+      num(a[6]), num(a[7]), dtype(a[0]))                                                                                  \
+    X(xnor_w4_linear_q8, 11, dense_of<int8_t>(a[0], c10::ScalarType::Char, area(a[5], a[6])),                             \
+      dense_f32(a[1], num(a[5]) * groups(num(a[6]), num(a[9]))),                                                          \
+      bytes(a[2], p_xnor_w4_wimg_bytes(num(a[7]), num(a[6]), num(a[8]))),                                                 \
+      dense(a[3], scalar_type(dtype(a[3])), area(a[5], a[7])),                                                            \
+      bytes(a[4], p_xnor_w4_linear_workspace_bytes(num(a[5]), num(a[6]), num(a[7]), num(a[8]))), num(a[5]), num(a[6]),    \
+      num(a[7]), num(a[8]), num(a[9]), dtype(a[3]))                                                                       \
+    X(xnor_logprobs, 14, rows(a[0], dtype(a[0]), num(a[9]), num(a[10])), stride(a[0], num(a[9]), num(a[10])),             \
+      tokens(a[1], area(a[9], a[11])), token_bytes(a[1]), dense_f32(a[2], area(a[9], a[11])), dense_f32(a[3], num(a[9])), \
+      dense_f32(a[4], 2 * (int64_t)num(a[9])), dense_f32(a[5], num(a[9])),                                                \
+      dense_of<int32_t>(a[6], c10::ScalarType::Int, area(a[9], a[12])), dense_f32(a[7], area(a[9], a[12])),               \
+      bytes(a[8], p_xnor_logprobs_workspace_bytes(num(a[9]), num(a[10]), num(a[12]))), num(a[9]), num(a[10]), num(a[11]), \
+      num(a[12]), dtype(a[0]))                                                                                            \
+    X(xnor_logprobs_backward, 11, rows(a[0], dtype(a[0]), num(a[7]), num(a[8])), stride(a[0], num(a[7]), num(a[8])),      \
+      tokens(a[1], area(a[7], a[9])), token_bytes(a[1]), dense_f32(a[2], 2 * (int64_t)num(a[7])),                         \
+      dense_f32(a[3], num(a[7])), dense_f32(a[4], area(a[7], a[9])), dense_f32(a[5], num(a[7])),                          \
+      dense(a[6], scalar_type(dtype(a[0])), area(a[7], a[8])), num(a[7]), num(a[8]), num(a[9]), dtype(a[0]))
 
 #define XNOR_POINTER(NAME, N, ...) decltype(&::NAME) p_##NAME = nullptr;
 XNOR_CALLS(XNOR_POINTER)
@@ -185,6 +302,8 @@ PyObject *bind(PyObject *, PyObject *args)
         return nullptr;                                                                 \
     }
     XNOR_CALLS(XNOR_LOOKUP)
+#define XNOR_QUERY_LOOKUP(NAME) XNOR_LOOKUP(NAME, 0)
+    XNOR_QUERIES(XNOR_QUERY_LOOKUP)
     Py_INCREF(raise); Py_INCREF(device); Py_INCREF(raw); Py_INCREF(desc);
     Py_XDECREF(g_raise); Py_XDECREF(g_current_device); Py_XDECREF(g_raw_stream); Py_XDECREF(g_desc);
     g_raise = raise; g_current_device = device; g_raw_stream = raw; g_desc = desc;

@@ -1,4 +1,4 @@
-"""Thin binding of libxnor (include/xnor.h): same names, argument marshalling only.  The calls that enqueue work go through
+"""Thin binding of libxnor (include/xnor.h, include/xnor_lowbit.h): same names, argument marshalling only.  The calls that enqueue work go through
 csrc/binding.cpp, queries through ctypes.
 
 Tensors are torch CUDA tensors used as plain device buffers; every step of the path runs in
@@ -28,7 +28,11 @@ EXPORTS = ["xnor_words_per_pixel", "xnor_output_hw", "xnor_status_string", "xnor
            "xnor_bingrad_pack_weights", "xnor_bingrad_binarize", "xnor_bingrad_conv2d",
            "xnor_conv2d_pool", "xnor_pool_fusion_choice",
            "xnor_kbit_input_bytes", "xnor_kbit_wimg_bytes", "xnor_kbit_pack_input", "xnor_kbit_pack_weights",
-           "xnor_kbit_conv2d"]
+           "xnor_kbit_conv2d",
+           "xnor_rmsnorm_q8", "xnor_rmsnorm_backward_workspace_bytes", "xnor_rmsnorm_backward",
+           "xnor_w4_quantize", "xnor_w4_wimg_bytes", "xnor_w4_pack", "xnor_w4_linear_workspace_bytes", "xnor_w4_linear",
+           "xnor_w4_linear_q8",
+           "xnor_logprobs_workspace_bytes", "xnor_logprobs", "xnor_logprobs_backward"]
 
 
 class XnorError(RuntimeError):
@@ -118,6 +122,22 @@ def lib():
         L.xnor_kbit_pack_weights.restype = ip
         L.xnor_kbit_conv2d.argtypes = [vp] * 5 + [ctypes.POINTER(ConvDesc), ip, ip, vp]
         L.xnor_kbit_conv2d.restype = ip
+        ll, fl, size = ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
+        for name, args, res in (
+                ("xnor_rmsnorm_q8", [vp, ll, vp, ll] + [vp] * 6 + [ip] * 4 + [fl, vp], ip),
+                ("xnor_rmsnorm_backward_workspace_bytes", [ip] * 2, size),
+                ("xnor_rmsnorm_backward", [vp, ll, vp, vp, vp, ll, vp, ll, vp, vp, vp] + [ip] * 3 + [vp], ip),
+                ("xnor_w4_quantize", [vp, ll, vp, vp, vp] + [ip] * 4 + [vp], ip),
+                ("xnor_w4_wimg_bytes", [ip] * 3, size),
+                ("xnor_w4_pack", [vp] * 4 + [ip] * 3 + [vp], ip),
+                ("xnor_w4_linear_workspace_bytes", [ip] * 4, size),
+                ("xnor_w4_linear", [vp, ll, vp, vp, vp] + [ip] * 5 + [vp], ip),
+                ("xnor_w4_linear_q8", [vp] * 5 + [ip] * 6 + [vp], ip),
+                ("xnor_logprobs_workspace_bytes", [ip] * 3, size),
+                ("xnor_logprobs", [vp, ll, vp, ip] + [vp] * 7 + [ip] * 5 + [vp], ip),
+                ("xnor_logprobs_backward", [vp, ll, vp, ip] + [vp] * 5 + [ip] * 4 + [vp], ip)):
+            getattr(L, name).argtypes = args
+            getattr(L, name).restype = res
         _lib = L
     return _lib
 
@@ -284,6 +304,55 @@ def xnor_kbit_conv2d(xq, wq, scale, out, num_out, desc, ka, kw_bits, stream=None
     _call.xnor_kbit_conv2d(xq, wq, scale, out, num_out, desc, int(ka), int(kw_bits), stream)
 
 
+# ---- include/xnor_lowbit.h: tensors of float32, bfloat16 or float16 carry their type, matrices their rows' distance -------
+def xnor_rmsnorm_q8(x, residual, weight, sum_out, q, scale, values, rstd, rows, cols, group, eps, stream=None):
+    _call.xnor_rmsnorm_q8(x, residual, weight, sum_out, q, scale, values, rstd, rows, cols, group, eps, stream)
+
+
+def rmsnorm_backward_workspace_bytes(rows, cols):
+    return int(lib().xnor_rmsnorm_backward_workspace_bytes(rows, cols))
+
+
+def xnor_rmsnorm_backward(h, rstd, weight, g_values, g_sum, g_h, g_weight, workspace, rows, cols, stream=None):
+    _call.xnor_rmsnorm_backward(h, rstd, weight, g_values, g_sum, g_h, g_weight, workspace, rows, cols, stream)
+
+
+def xnor_w4_quantize(w, codes, scale, zero, out_features, in_features, group, stream=None):
+    _call.xnor_w4_quantize(w, codes, scale, zero, out_features, in_features, group, stream)
+
+
+def w4_wimg_bytes(out_features, in_features, group):
+    return int(lib().xnor_w4_wimg_bytes(out_features, in_features, group))
+
+
+def xnor_w4_pack(codes, scale, zero, wimg, out_features, in_features, group, stream=None):
+    _call.xnor_w4_pack(codes, scale, zero, wimg, out_features, in_features, group, stream)
+
+
+def w4_linear_workspace_bytes(rows, in_features, out_features, group):
+    return int(lib().xnor_w4_linear_workspace_bytes(rows, in_features, out_features, group))
+
+
+def xnor_w4_linear(x, wimg, y, workspace, rows, in_features, out_features, group, stream=None):
+    _call.xnor_w4_linear(x, wimg, y, workspace, rows, in_features, out_features, group, stream)
+
+
+def xnor_w4_linear_q8(q, x_scale, wimg, y, workspace, rows, in_features, out_features, group, x_group, stream=None):
+    _call.xnor_w4_linear_q8(q, x_scale, wimg, y, workspace, rows, in_features, out_features, group, x_group, stream)
+
+
+def logprobs_workspace_bytes(rows, vocab, top):
+    return int(lib().xnor_logprobs_workspace_bytes(rows, vocab, top))
+
+
+def xnor_logprobs(logits, tokens, logprob, lse, shift, entropy, top_index, top_logprob, workspace, rows, vocab, given, top, stream=None):
+    _call.xnor_logprobs(logits, tokens, logprob, lse, shift, entropy, top_index, top_logprob, workspace, rows, vocab, given, top, stream)
+
+
+def xnor_logprobs_backward(logits, tokens, shift, entropy, g_logprob, g_entropy, g_logits, rows, vocab, given, stream=None):
+    _call.xnor_logprobs_backward(logits, tokens, shift, entropy, g_logprob, g_entropy, g_logits, rows, vocab, given, stream)
+
+
 def xnor_pack_weights(w, wbits, alpha, wmfma, k_out, c, kh, kw, stream=None):
     _call.xnor_pack_weights(w, wbits, alpha, wmfma, k_out, c, kh, kw, stream)
 
@@ -336,6 +405,27 @@ class PackedWeights:
         self.wmfma = (torch.empty((wmfma_bytes(k_out, c, kh, kw),), dtype=torch.uint8, device=device)
                       if with_mfma else None)
         xnor_pack_weights(w, self.wbits, self.alpha, self.wmfma, k_out, c, kh, kw, stream)
+
+
+class W4Weights:
+    """The image of 4-bit weights that the products read (`wimg`), packed from codes, scale and zero (None: 8 everywhere)."""
+
+    def __init__(self, codes, scale, zero, in_features, group, stream=None):
+        out_features = codes.shape[0]
+        self.shape, self.group = (out_features, in_features), group
+        self.wimg = torch.empty((w4_wimg_bytes(out_features, in_features, group),), dtype=torch.uint8, device=codes.device)
+        xnor_w4_pack(codes, scale, zero, self.wimg, out_features, in_features, group, stream)
+
+    @classmethod
+    def quantized(cls, w, group, zeros=False, stream=None):
+        """From real weights [out][in], rounded by xnor_w4_quantize (zeros: with zero points)."""
+        out_features, in_features = w.shape
+        groups = -(-in_features // group)
+        codes = torch.empty((out_features, 16 * -(-in_features // 32)), dtype=torch.uint8, device=w.device)
+        scale = torch.empty((out_features, groups), dtype=torch.float32, device=w.device)
+        zero = torch.empty((out_features, groups), dtype=torch.uint8, device=w.device) if zeros else None
+        xnor_w4_quantize(w, codes, scale, zero, out_features, in_features, group, stream)
+        return cls(codes, scale, zero, in_features, group, stream)
 
 
 class ConvBuffers:
