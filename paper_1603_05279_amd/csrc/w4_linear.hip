@@ -2,6 +2,7 @@
 #include "xnor_internal.h"
 #include "real8.h"
 #include "lowbit.h"
+#include "w4_form.h"
 #include "w4_image.h"
 #include <algorithm>
 
@@ -82,114 +83,6 @@ __global__ __launch_bounds__(256) void w4_pack_kernel(const uint32_t *codes, con
 
 // ---- products -----------------------------------------------------------------------------------------------------------
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-
-// How rows meet the codes in the matrix instructions (16 x 16 x 32).  A code u enters as a number that takes two instructions per pair to
-// form: 16 + u in 16 bits, where it is the top of the mantissa under a fixed exponent, u in 8 bits.  What that and the zero point add to a
-// sum is the same multiple of the group's sum of x for all inputs; another product, by ones, makes that sum in the same registers:
-//     sum x (u - z) = sum x (OFFSET + u) - (OFFSET + z) sum x
-// Float32 rows are three bfloat16 numbers each whose sum they are.
-enum { ROWS_F32 = XNOR_F32, ROWS_BF16 = XNOR_BF16, ROWS_F16 = XNOR_F16, ROWS_I8 = 3 };
-
-template <int X> struct Form {          // 16 bits
-    static constexpr int PARTS = X == ROWS_F32 ? 3 : 1;
-    static constexpr float OFFSET = 16.0f;
-    typedef f32x4 acc_t;
-    typedef u32x4 operand_t;
-    static __device__ __forceinline__ operand_t ones()
-    {
-        const uint32_t one = X == ROWS_F16 ? 0x3c003c00u : 0x3f803f80u;
-        return operand_t{one, one, one, one};
-    }
-    static __device__ __forceinline__ operand_t widen(uint32_t w)
-    {
-        if (X == ROWS_F16)
-            return operand_t{(w << 6 & 0x03c003c0u) | 0x4c004c00u, (w << 2 & 0x03c003c0u) | 0x4c004c00u, (w >> 2 & 0x03c003c0u) | 0x4c004c00u,
-                             (w >> 6 & 0x03c003c0u) | 0x4c004c00u};
-        return operand_t{(w << 3 & 0x00780078u) | 0x41804180u, (w >> 1 & 0x00780078u) | 0x41804180u, (w >> 5 & 0x00780078u) | 0x41804180u,
-                         (w >> 9 & 0x00780078u) | 0x41804180u};
-    }
-    static __device__ __forceinline__ acc_t mfma(operand_t a, operand_t b, acc_t c)
-    {
-        if (X == ROWS_F16)
-            return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-    }
-};
-template <> struct Form<ROWS_I8> {
-    static constexpr int PARTS = 1;
-    typedef i32x4 acc_t;
-    typedef long operand_t;             // bytes 0 4 1 5 2 6 3 7 of eight neighbours
-    static __device__ __forceinline__ operand_t ones() { return 0x0101010101010101l; }
-    static __device__ __forceinline__ operand_t widen(uint32_t w)
-    {
-        return (operand_t)((uint64_t)(w & 0x0f0f0f0fu) | (uint64_t)(w >> 4 & 0x0f0f0f0fu) << 32);
-    }
-    static __device__ __forceinline__ acc_t mfma(operand_t a, operand_t b, acc_t c) { return __builtin_amdgcn_mfma_i32_16x16x32_i8(a, b, c, 0, 0, 0); }
-};
-
-// Eight neighbours of a row as operands (PARTS of them); n: how many exist, the others are 0.
-template <int X> struct Eight;
-template <int X> struct Eight {
-    Real8<X> v;
-    __device__ __forceinline__ void load(const void *row, int k, int n) { v.load(static_cast<const real_t<X> *>(row) + k, n); }
-    __device__ __forceinline__ void operands(typename Form<X>::operand_t *b) const
-    {
-        if constexpr (X != ROWS_F32) {
-            b[0] = v.quad[0];
-        } else {
-            // truncated to 8 bits of mantissa, then the rest, and the rest of that: exact (an infinity has no rest, a NaN stays one)
-            uint32_t w[3][4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t part[2][3];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float x = v[2 * i + h];
-                    const bool finite = __builtin_fabsf(x) < __builtin_inff();
-                    const uint32_t hi = (__float_as_uint(x) | (x != x ? 0x00400000u : 0u)) & 0xffff0000u;
-                    const float rest = finite ? x - __uint_as_float(hi) : 0.0f;
-                    const uint32_t mid = __float_as_uint(rest) & 0xffff0000u;
-                    part[h][0] = hi;
-                    part[h][1] = mid;
-                    part[h][2] = __float_as_uint(rest - __uint_as_float(mid));
-                }
-#pragma unroll
-                for (int p = 0; p < 3; ++p) w[p][i] = part[0][p] >> 16 | (part[1][p] & 0xffff0000u);
-            }
-#pragma unroll
-            for (int p = 0; p < 3; ++p) b[p] = u32x4{w[p][0], w[p][1], w[p][2], w[p][3]};
-        }
-    }
-};
-template <> struct Eight<ROWS_I8> {
-    uint32_t w[2];
-    __device__ __forceinline__ void load(const void *row, int k, int n)
-    {
-        const int8_t *p = static_cast<const int8_t *>(row) + k;
-        if (n >= 8) {
-            typedef uint32_t words2 __attribute__((ext_vector_type(2), aligned(1)));
-            const words2 v = *reinterpret_cast<const words2 *>(p);
-            w[0] = v.x;
-            w[1] = v.y;
-        } else {
-            w[0] = w[1] = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < n) w[i / 4] |= (uint32_t)(uint8_t)p[i] << (8 * (i & 3));
-        }
-    }
-    __device__ __forceinline__ void operands(long *b) const
-    {
-        const uint32_t lo = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), hi = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u);
-        b[0] = (long)((uint64_t)lo | (uint64_t)hi << 32);
-    }
-};
-
 struct W4Args {
     const void *x;
     const float *x_scale;
@@ -213,7 +106,7 @@ __global__ __launch_bounds__(64 * WAVES) void w4_rows_kernel(W4Args a)
     const int tile = blockIdx.x, row0 = blockIdx.y * 16 * BLOCKS;
     const u32x4 *codes = reinterpret_cast<const u32x4 *>(a.image) + (size_t)tile * l.chunks * 64 + lane;
     const float *scales = reinterpret_cast<const float *>(a.image + l.scale_at()) + (size_t)tile * l.groups * 16 + 4 * quarter;
-    const uint8_t *zeros = a.image + l.zero_at() + (size_t)tile * l.groups * 16 + 4 * quarter;
+    const uint8_t *zeros = a.image + l.zero_at() + (size_t)tile * l.groups * 16 + (X == ROWS_I8 ? col : 4 * quarter);
     const char *xrow[BLOCKS];
     bool real[BLOCKS];
     constexpr int XBYTES = X == ROWS_F32 ? 4 : X == ROWS_I8 ? 1 : 2;
@@ -238,35 +131,42 @@ __global__ __launch_bounds__(64 * WAVES) void w4_rows_kernel(W4Args a)
                 x[j][b].load(xrow[b], k, real[b] ? a.in - k : 0);
             }
         typename F::acc_t acc[BLOCKS], sum[BLOCKS];
+        uint32_t zero = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int k0 = 128 * chunk + 32 * j;
-            if (j % steps_per_group == 0)
+            const int k0 = 128 * chunk + 32 * j, g = min(k0 / a.group, l.groups - 1);
+            if (j % steps_per_group == 0) {
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b) acc[b] = sum[b] = typename F::acc_t{0, 0, 0, 0};
-            const auto wide = F::widen(w[j]);
+                if (X == ROWS_I8) zero = zeros[(size_t)g * 16] * 0x01010101u;
+            }
 #pragma unroll
             for (int b = 0; b < BLOCKS; ++b) {
                 typename F::operand_t xo[F::PARTS];
                 x[j][b].operands(xo);
+                if constexpr (X == ROWS_I8) {
+                    acc[b] = F::mfma(F::widen(w[j], zero), xo[0], acc[b]);
+                } else {
 #pragma unroll
-                for (int p = 0; p < F::PARTS; ++p) {
-                    acc[b] = F::mfma(wide, xo[p], acc[b]);
-                    sum[b] = F::mfma(F::ones(), xo[p], sum[b]);
+                    for (int p = 0; p < F::PARTS; ++p) {
+                        acc[b] = F::mfma(F::widen(w[j]), xo[p], acc[b]);
+                        sum[b] = F::mfma(F::ones(), xo[p], sum[b]);
+                    }
                 }
             }
-            if ((j + 1) % steps_per_group == 0 && k0 + 32 - a.group < a.in) {
-                const int g = k0 / a.group;
+            if ((j + 1) % steps_per_group == 0) {           // (a group past the last input has sums of zero)
                 const f32x4 s = *reinterpret_cast<const f32x4 *>(scales + (size_t)g * 16);
-                const uint32_t z = *reinterpret_cast<const uint32_t *>(zeros + (size_t)g * 16);
+                uint32_t z = 0;
+                if constexpr (X != ROWS_I8) z = *reinterpret_cast<const uint32_t *>(zeros + (size_t)g * 16);
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b) {
                     float xs = 1.0f;
-                    if (X == ROWS_I8 && a.x_group) xs = a.x_scale[(size_t)min(row0 + 16 * b + col, a.rows - 1) * a.x_groups + k0 / a.x_group];
+                    if (X == ROWS_I8 && a.x_group)
+                        xs = a.x_scale[(size_t)min(row0 + 16 * b + col, a.rows - 1) * a.x_groups + min(k0 / a.x_group, a.x_groups - 1)];
 #pragma unroll
                     for (int v = 0; v < 4; ++v) {
                         float part;
-                        if constexpr (X == ROWS_I8) part = (float)(acc[b][v] - (int)(z >> (8 * v) & 255u) * sum[b][v]) * xs;
+                        if constexpr (X == ROWS_I8) part = (float)acc[b][v] * xs;
                         else part = __builtin_fmaf(-(F::OFFSET + (float)(z >> (8 * v) & 255u)), sum[b][v], acc[b][v]);
                         total[b][v] = __builtin_fmaf(s[v], part, total[b][v]);
                     }
@@ -323,11 +223,15 @@ xnor_status launch_w4_pack(const uint8_t *codes, const float *scale, const uint8
     return hip_status(hipGetLastError());
 }
 
-size_t w4_linear_workspace_bytes(int rows, int in, int out, int group) { return 0; }
+size_t w4_linear_workspace_bytes(int rows, int in, int out, int group)
+{
+    return w4_tiles_applies(rows) ? w4_tiles_workspace_bytes(rows, in, out, group) : 0;
+}
 
 xnor_status launch_w4_linear(const void *x, long long x_stride, const void *wimg, void *y, void *workspace, int rows, int in, int out, int group, int type,
                              hipStream_t stream)
 {
+    if (w4_tiles_applies(rows)) return launch_w4_tiles(x, x_stride, nullptr, wimg, y, workspace, rows, in, out, group, 0, type, type, stream);
     const W4Args a{x, nullptr, static_cast<const uint8_t *>(wimg), y, x_stride, rows, in, out, group, 0, 1};
     by_type(type, [&](auto t) { launch_rows<t(), t()>(a, stream); });
     return hip_status(hipGetLastError());
@@ -336,6 +240,7 @@ xnor_status launch_w4_linear(const void *x, long long x_stride, const void *wimg
 xnor_status launch_w4_linear_q8(const int8_t *q, const float *x_scale, const void *wimg, void *y, void *workspace, int rows, int in, int out, int group,
                                 int x_group, int type, hipStream_t stream)
 {
+    if (w4_tiles_applies(rows)) return launch_w4_tiles(q, in, x_scale, wimg, y, workspace, rows, in, out, group, x_group, ROWS_I8, type, stream);
     const W4Args a{q, x_scale, static_cast<const uint8_t *>(wimg), y, in, rows, in, out, group, x_group, x_group ? (in + x_group - 1) / x_group : 1};
     by_type(type, [&](auto t) { launch_rows<ROWS_I8, t()>(a, stream); });
     return hip_status(hipGetLastError());
