@@ -10,7 +10,7 @@ namespace {
 
 constexpr int THREADS = 256, STEPS = 4, CHUNK = THREADS * 8 * STEPS;      // logits that a workgroup holds in registers at a time
 constexpr int GROUP_LANES = 4, GROUPS = THREADS / GROUP_LANES;            // threads whose largest logits are compared as one
-constexpr float LOG2E = 1.44269504088896340736f;
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.693147180559945309417f;
 
 // A running softmax: the largest logit m, s = sum exp(l - m) and t = sum exp(l - m) (l - m); entropy = log s - t / s.  The terms of t are
 // differences, so masks of any magnitude leave it finite.
@@ -18,27 +18,25 @@ struct Stats {
     float m, s, t;
 };
 __device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * LOG2E); }
-__device__ __forceinline__ void rescale(Stats &a, float m)
+// s and t of a, whose largest is a.m, for a largest logit m >= a.m instead
+__device__ __forceinline__ Stats rescaled(Stats a, float m)
 {
-    const float d = a.m - m;
-    if (d != 0.0f) {                                    // (NaN: -inf on both sides, and nothing summed yet)
-        const float f = exp_of(d);
-        a.t = f > 0.0f ? f * (a.t + d * a.s) : 0.0f;
-        a.s = f > 0.0f ? f * a.s : a.s != a.s ? a.s : 0.0f;
-    }
-    a.m = m;
+    const float d = a.m - m, f = exp_of(d);
+    const bool some = d > -100.0f;                      // (else nothing is left of it, or nothing was summed: -inf on both sides)
+    return {m, some ? f * a.s : a.s != a.s ? a.s : 0.0f, some ? f * __builtin_fmaf(d, a.s, a.t) : 0.0f};
 }
-__device__ __forceinline__ Stats merged(Stats a, Stats b)
-{
-    const float m = fmaxf(a.m, b.m);
-    rescale(a, m);
-    rescale(b, m);
-    return {m, a.s + b.s, a.t + b.t};
-}
+// Statistics of a wave in all its lanes.
 __device__ __forceinline__ Stats wave_merged(Stats a)
 {
+    float m = a.m;
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) a = merged(a, {__shfl_xor(a.m, d, 64), __shfl_xor(a.s, d, 64), __shfl_xor(a.t, d, 64)});
+    for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+    a = rescaled(a, m);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+        a.s += __shfl_xor(a.s, d, 64);
+        a.t += __shfl_xor(a.t, d, 64);
+    }
     return a;
 }
 
@@ -60,74 +58,92 @@ __device__ __forceinline__ key_t none_key() { return key_of(-__builtin_inff(), 0
 struct TopLds {
     key_t list[32];             // the best so far, in order; filled up with none_key()
     key_t group[GROUPS];
-    int count;
-    key_t found[];              // up to top * GROUP_LANES * (keys per thread)
+    uint32_t short_group[GROUPS];
+    int count;                  // 0 between uses
+    key_t found[];              // up to 32 + top * GROUP_LANES * (keys per thread)
 };
 
-// The top-th largest of the groups' largest keys (every wave finds it by itself): at least `top` keys are not below it, and those that are
-// not belong to `top` groups.
-__device__ __forceinline__ key_t group_threshold(TopLds &t, key_t mine, int top)
+// The upper half of a key with 6 bits less, and in their place the group's number: short keys that differ.
+__device__ __forceinline__ uint32_t short_key(uint32_t upper, int group) { return (upper & ~63u) | (uint32_t)(63 - group); }
+
+// A value that at least `top` of the groups reach with their largest (t.short_group; every wave finds it by itself), as the upper half of a key.
+__device__ __forceinline__ uint32_t short_rank(const TopLds &t, int top)
+{
+    const uint32_t g = t.short_group[threadIdx.x & 63];
+    int rank = 0;
+#pragma unroll
+    for (int i = 0; i < GROUPS; i += 4) {
+        const uint4 o = *reinterpret_cast<const uint4 *>(t.short_group + i);
+        rank += (o.x > g ? 1 : 0) + (o.y > g ? 1 : 0) + (o.z > g ? 1 : 0) + (o.w > g ? 1 : 0);
+    }
+    const int who = __builtin_ctzll(__ballot(rank == top - 1));
+    return (uint32_t)__builtin_amdgcn_readlane((int)g, who) & ~63u;
+}
+
+// The top-th largest of the 64 different keys in t.group (every wave finds it by itself).
+__device__ __forceinline__ key_t group_rank(const TopLds &t, int top)
 {
     const int lane = threadIdx.x & 63;
+    const key_t g = t.group[lane];
+    int rank = 0;
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+        const key_t o = t.group[i];
+        rank += o > g ? 1 : 0;
+    }
+    const int who = __builtin_ctzll(__ballot(rank == top - 1));
+    return (key_t)__shfl((long long)g, who, 64);
+}
+// The top-th largest of the groups' largest keys: at least `top` keys are not below it, and those that are not belong to `top` groups.
+__device__ __forceinline__ key_t group_threshold(TopLds &t, key_t mine, int top)
+{
 #pragma unroll
     for (int d = 1; d < GROUP_LANES; d <<= 1) {
         const key_t o = (key_t)__shfl_xor((long long)mine, d, 64);
         mine = o > mine ? o : mine;
     }
+    if (threadIdx.x % GROUP_LANES == 0) t.group[threadIdx.x / GROUP_LANES] = mine ? mine : threadIdx.x;        // (a key of its own, below all others)
     __syncthreads();
-    if (threadIdx.x % GROUP_LANES == 0) t.group[threadIdx.x / GROUP_LANES] = mine;
-    __syncthreads();
-    const key_t g = t.group[lane];
-    int rank = 0;
-#pragma unroll 16
-    for (int i = 0; i < GROUPS; ++i) {
-        const key_t o = t.group[i];
-        rank += o > g || (o == g && i < lane) ? 1 : 0;
-    }
-    const int who = __builtin_ctzll(__ballot(rank == top - 1));
-    return (key_t)__shfl((long long)g, who, 64);
+    return group_rank(t, top);
 }
 
-// list = the `top` largest of list and found[0 .. n); called by all threads, found and n settled behind a barrier.
-__device__ void select_top(TopLds &t, int n, int top)
+// list = the `top` largest of found[0 .. n), in order; called by all threads, found and n settled behind a barrier.
+__device__ __forceinline__ void select_top(TopLds &t, int n, int top)
 {
     // a long list is thinned out first: 32 of 64 groups can hold what is not below the threshold, so its length falls to half or less
     while (n > THREADS) {
+        constexpr int MOST = (32 + 32 * GROUP_LANES * 32 + THREADS - 1) / THREADS;
         key_t best = 0;
         for (int i = threadIdx.x; i < n; i += THREADS) best = max(best, t.found[i]);
+        __syncthreads();                                        // (t.group is read no more)
         const key_t least = group_threshold(t, best, top);
-        constexpr int MOST = 32 * GROUP_LANES * 32 / THREADS;
-        key_t mine[MOST];
-        int have = 0;
-#pragma unroll
+        uint32_t keep = 0;
         for (int i = 0; i < MOST; ++i) {
             const int at = threadIdx.x + i * THREADS;
-            mine[i] = at < n ? t.found[at] : 0;
-            have += mine[i] >= least ? 1 : 0;
+            if (at < n && t.found[at] >= least) keep |= 1u << i;
         }
         if (threadIdx.x == 0) t.count = 0;
         __syncthreads();
-        int at = have ? atomicAdd(&t.count, have) : 0;
-#pragma unroll
-        for (int i = 0; i < MOST; ++i)
-            if (mine[i] >= least) t.found[at++] = mine[i];
-        __syncthreads();
+        // moved to places below their own or that others have left: through registers, a round of places at a time
+        for (int i = 0; i * THREADS < n; ++i) {
+            const bool mine = keep >> i & 1u;
+            const key_t k = mine ? t.found[threadIdx.x + i * THREADS] : 0;
+            __syncthreads();
+            if (mine) t.found[atomicAdd(&t.count, 1)] = k;
+            __syncthreads();
+        }
         n = t.count;
         __syncthreads();
     }
     // ranks by counting: keys differ, so every rank is taken once
     const int i = threadIdx.x;
-    const key_t old = i < top ? t.list[i] : 0, neu = i < n ? t.found[i] : 0;
-    int rank_old = i, rank_new = 0;
-    for (int j = 0; j < n; ++j) {
-        const key_t o = t.found[j];
-        rank_old += o > old ? 1 : 0;
-        rank_new += o > neu ? 1 : 0;
-    }
-    for (int j = 0; j < top; ++j) rank_new += t.list[j] > neu ? 1 : 0;
-    __syncthreads();
-    if (i < top && rank_old < top) t.list[rank_old] = old;
-    if (i < n && rank_new < top) t.list[rank_new] = neu;
+    const key_t mine = i < n ? t.found[i] : 0;
+    int rank = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) rank += t.found[j] > mine ? 1 : 0;
+    if (i < n && rank < top) t.list[rank] = max(mine, none_key());
+    if (i >= n && i < top) t.list[i] = none_key();
+    if (i == 0) t.count = 0;
     __syncthreads();
 }
 
@@ -147,12 +163,23 @@ __device__ __forceinline__ long long token_at(const void *tokens, int bytes, siz
     return bytes == 8 ? static_cast<const long long *>(tokens)[i] : (long long)static_cast<const int32_t *>(tokens)[i];
 }
 
+// The logit of a thread's own given token, fetched while the row is read.
+struct Given {
+    bool real;
+    float logit;
+};
+template <int TYPE> __device__ __forceinline__ Given given_at(const LogprobArgs &a, size_t row, int i)
+{
+    if (i >= a.given) return {false, 0.0f};
+    const long long token = token_at(a.tokens, a.token_bytes, row * a.given + i);
+    const bool real = token >= 0 && token < a.vocab;
+    return {real, real ? (float)(static_cast<const real_t<TYPE> *>(a.logits) + row * (size_t)a.stride)[token] : 0.0f};
+}
+
 // A row's results from its statistics and the list of alternatives (all threads of the workgroup).
 template <int TYPE>
-__device__ void finish_row(const LogprobArgs &a, size_t row, Stats st, const key_t *list)
+__device__ __forceinline__ void finish_row(const LogprobArgs &a, size_t row, Stats st, const key_t *list, Given own)
 {
-    typedef real_t<TYPE> T;
-    const T *l = static_cast<const T *>(a.logits) + row * (size_t)a.stride;
     const bool empty = st.m == -__builtin_inff() && !(st.s != st.s);
     const float log_s = empty ? 0.0f : __builtin_logf(st.s), base = empty ? 0.0f : st.m;
     if (threadIdx.x == 0) {
@@ -163,11 +190,12 @@ __device__ void finish_row(const LogprobArgs &a, size_t row, Stats st, const key
         }
         if (a.entropy) a.entropy[row] = empty ? 0.0f : log_s - st.t / st.s;
     }
-    for (int i = threadIdx.x; i < a.given; i += blockDim.x) {
-        const long long token = token_at(a.tokens, a.token_bytes, row * a.given + i);
-        a.logprob[row * a.given + i] = token >= 0 && token < a.vocab ? ((float)l[token] - base) - log_s : 0.0f;
+    for (int i = threadIdx.x; i < a.given; i += THREADS) {
+        if (i >= THREADS) own = given_at<TYPE>(a, row, i);
+        a.logprob[row * a.given + i] = own.real ? (own.logit - base) - log_s : 0.0f;
     }
-    for (int i = threadIdx.x; i < a.top; i += blockDim.x) {
+    const int i = threadIdx.x;
+    if (i < a.top) {
         const bool real = list[i] > none_key() && log_s == log_s;
         a.top_index[row * a.top + i] = real ? (int32_t)index_of(list[i]) : -1;
         a.top_logprob[row * a.top + i] = real ? (value_of(list[i]) - base) - log_s : log_s == log_s ? -__builtin_inff() : log_s;
@@ -191,106 +219,178 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobArgs a)
     const T *l = static_cast<const T *>(a.logits) + row * (size_t)a.stride;
     if (TOP) {
         if (tid < 32) top.list[tid] = none_key();
+        if (tid == 0) top.count = 0;
         __syncthreads();
     }
+    const Given own = a.parts == 1 ? given_at<TYPE>(a, row, tid) : Given{false, 0.0f};
     Stats st{-__builtin_inff(), 0.0f, 0.0f};
     Real8<TYPE> next[STEPS];
-    auto fetch = [&](int c0) {
+    auto load_chunk = [&](Real8<TYPE> *v, int c0) {
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
             const int c = c0 + 8 * (tid + i * THREADS);
-            next[i].load(l + c, last - c, -__builtin_inff());
+            v[i].load(l + c, last - c, -__builtin_inff());
         }
     };
-    fetch(first);
+    load_chunk(next, first);
     for (int c0 = first; c0 < last; c0 += CHUNK) {
-        Real8<TYPE> raw[STEPS];
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) raw[i] = next[i];
-        if (c0 + CHUNK < last) fetch(c0 + CHUNK);
         float m = -__builtin_inff();
+        Real8<TYPE> raw[STEPS];
+        {
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i)
+            for (int i = 0; i < STEPS; ++i) raw[i] = next[i];
+            if (c0 + CHUNK < last) load_chunk(next, c0 + CHUNK);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) m = fmaxf(m, raw[i][j]);
-        if (m > st.m) rescale(st, m);
-        const float base = st.m == -__builtin_inff() ? 0.0f : st.m;
+            for (int i = 0; i < STEPS; ++i)
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float d = raw[i][j] - base, e = exp_of(d);
-                st.s += e;
-                if (ENTROPY) st.t = __builtin_fmaf(e, fmaxf(d, -200.0f), st.t);      // (e = 0 from there on, also for -inf)
-            }
-        if (TOP) {
-            key_t least = top.list[a.top - 1];
-            float least_value = value_of(least);
-            const int over = __syncthreads_count(m > least_value);
-            if (over == 0) continue;
-            if (over > GROUP_LANES * a.top) {
-                uint32_t at = 0;
-#pragma unroll
-                for (int i = STEPS - 1; i >= 0; --i)
-#pragma unroll
-                    for (int j = 7; j >= 0; --j) at = raw[i][j] == m ? (uint32_t)(8 * i * THREADS + j) : at;
-                const key_t least_here = group_threshold(top, m > least_value ? key_of(m, (uint32_t)(c0 + 8 * tid) + at) : 0, a.top);
-                least = max(least, least_here - 1);                        // (keys above it are wanted)
-                least_value = value_of(least);
-            }
-            if (tid == 0) top.count = 0;
-            __syncthreads();
-            if (m >= least_value)
+                for (int j = 0; j < 8; ++j) m = fmaxf(m, raw[i][j]);
+            if (m > st.m) st = rescaled(st, m);
+            if (__builtin_fabsf(st.m) < 1024.0f) {
+                // in powers of 2, one operation for the difference: exp(l - m) = 2^(l c - m c) with c = log2 e.  m c rounds; what it lost (below
+                // 2^-13 here) is one factor of all terms, 1 - lost log 2 to 2^-27
+                const float mc = st.m * LOG2E, lost = __builtin_fmaf(st.m, LOG2E, -mc);
+                float s[2] = {0.0f, 0.0f}, t[2] = {0.0f, 0.0f};
 #pragma unroll
                 for (int i = 0; i < STEPS; ++i)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const float v = raw[i][j];
-                        if (v >= least_value) {
-                            const key_t k = key_of(v, (uint32_t)(c0 + 8 * (tid + i * THREADS) + j));
-                            if (k > least) top.found[atomicAdd(&top.count, 1)] = k;
-                        }
+                        const float d = __builtin_fmaf(raw[i][j], LOG2E, -mc), e = __builtin_amdgcn_exp2f(d);
+                        s[j & 1] += e;
+                        if (ENTROPY) t[j & 1] = __builtin_fmaf(e, fmaxf(d, -300.0f), t[j & 1]);      // (e = 0 from there on, also for -inf)
                     }
+                const float some = s[0] + s[1], back = 1.0f - lost * LN2;
+                st.s = __builtin_fmaf(some, back, st.s);
+                if (ENTROPY) st.t = __builtin_fmaf((t[0] + t[1] - lost * some) * LN2, back, st.t);
+            } else {                                                // (only masks so far, or logits of an unusual size)
+                const float base = st.m == -__builtin_inff() ? 0.0f : st.m;
+#pragma unroll
+                for (int i = 0; i < STEPS; ++i)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float d = raw[i][j] - base, e = exp_of(d);
+                        st.s += e;
+                        if (ENTROPY) st.t = __builtin_fmaf(e, fmaxf(d, -200.0f), st.t);
+                    }
+            }
+        }
+        if (TOP) {
+            const key_t last_key = top.list[a.top - 1];
+            float floor_value = value_of(last_key);
+            const int over = __syncthreads_count(m > floor_value);
+            if (over == 0) continue;
+            if (over > GROUP_LANES * a.top) {
+                uint32_t most = (uint32_t)(key_of(m, 0) >> 32);
+#pragma unroll
+                for (int d = 1; d < GROUP_LANES; d <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d, 64));
+                if (tid % GROUP_LANES == 0) top.short_group[tid / GROUP_LANES] = short_key(most, tid / GROUP_LANES);
+                __syncthreads();
+                floor_value = fmaxf(floor_value, value_of((key_t)short_rank(top, a.top) << 32));
+            }
+            floor_value = fmaxf(floor_value, -3.402823466e38f);             // (-inf is no alternative)
+            // one bit per logit; the few that are taken are read once more, from the cache (short code: most rows run it once)
+            static_assert(8 * STEPS == 32, "");
+            uint32_t taken = 0;
+            if (m >= floor_value)
+#pragma unroll
+                for (int i = 0; i < STEPS; ++i)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) taken |= raw[i][j] >= floor_value ? 1u << (8 * i + j) : 0;
+            auto logit = [&](int bit, uint32_t *index) {
+                *index = (uint32_t)(c0 + 8 * (tid + (bit >> 3) * THREADS) + (bit & 7));
+                return (float)l[*index];
+            };
+            int at = taken ? atomicAdd(&top.count, __builtin_popcount(taken)) : 0;
             __syncthreads();
-            select_top(top, top.count, a.top);
+            int n = top.count;
+            if (n <= a.top * GROUP_LANES * 8 * STEPS) {
+                for (; taken; taken &= taken - 1, ++at) {
+                    uint32_t index;
+                    const float v = logit(__builtin_ctz(taken), &index);
+                    const key_t k = key_of(v, index);
+                    top.found[at] = k > last_key ? k : (key_t)at;
+                }
+            } else {
+                // so many equal logits that they overflow the list: with their indices for order, as many as one list's worth are left
+                key_t best = 0;
+                for (uint32_t bits = taken; bits; bits &= bits - 1) {
+                    uint32_t index;
+                    const float v = logit(__builtin_ctz(bits), &index);
+                    best = max(best, key_of(v, index));
+                }
+                const key_t least = max(group_threshold(top, best > last_key ? best : 0, a.top), last_key + 1);
+                if (tid == 0) top.count = 0;
+                __syncthreads();
+                for (; taken; taken &= taken - 1) {
+                    uint32_t index;
+                    const float v = logit(__builtin_ctz(taken), &index);
+                    const key_t k = key_of(v, index);
+                    if (k >= least) top.found[atomicAdd(&top.count, 1)] = k;
+                }
+                __syncthreads();
+                n = top.count;
+            }
+            if (tid < a.top) top.found[n + tid] = top.list[tid] > none_key() ? top.list[tid] : (key_t)(n + tid);
+            __syncthreads();
+            select_top(top, n + a.top, a.top);
         }
     }
     st = wave_merged(st);
     if ((tid & 63) == 0) wave_stats[tid >> 6] = st;
     __syncthreads();
-    st = wave_stats[0];
+    {
+        float m = wave_stats[0].m, s = 0.0f, t = 0.0f;
 #pragma unroll
-    for (int i = 1; i < THREADS / 64; ++i) st = merged(st, wave_stats[i]);
+        for (int i = 1; i < THREADS / 64; ++i) m = fmaxf(m, wave_stats[i].m);
+#pragma unroll
+        for (int i = 0; i < THREADS / 64; ++i) {
+            const Stats w = rescaled(wave_stats[i], m);
+            s += w.s;
+            t += w.t;
+        }
+        st = {m, s, t};
+    }
     if (a.parts == 1) {
-        finish_row<TYPE>(a, row, st, top.list);
+        finish_row<TYPE>(a, row, st, top.list, own);
     } else {
         if (tid == 0) a.part_stats[blockIdx.x] = st;
         if (TOP && tid < a.top) a.part_top[(size_t)blockIdx.x * a.top + tid] = top.list[tid];
     }
 }
 
-// The parts of a row joined, in their order.
+// The parts of a row joined, in their order.  Each part's list is in order, so the first keys tell which lists can hold an alternative.
 template <int TYPE>
 __global__ __launch_bounds__(THREADS) void logprobs_join_kernel(LogprobArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     TopLds &top = *reinterpret_cast<TopLds *>(smem);
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, n = a.parts * a.top;
     const size_t row = blockIdx.x;
+    constexpr int MOST = 64 * 32 / THREADS;
     Stats st{-__builtin_inff(), 0.0f, 0.0f};
     if ((tid & 63) < a.parts) st = a.part_stats[row * a.parts + (tid & 63)];      // (every wave joins them all)
+    key_t first = none_key(), mine[MOST];
+    if (a.top) {
+        if (tid < a.parts) first = a.part_top[row * n + (size_t)tid * a.top];
+#pragma unroll
+        for (int i = 0; i < MOST; ++i) {
+            const int at = tid + i * THREADS;
+            mine[i] = at < n ? a.part_top[row * n + at] : 0;
+        }
+    }
+    const Given own = given_at<TYPE>(a, row, tid);
     st = wave_merged(st);
     if (a.top) {
-        if (tid < 32) top.list[tid] = none_key();
-        const int n = a.parts * a.top;
-        for (int i = tid; i < n; i += THREADS) {
-            const key_t k = a.part_top[row * n + i];
-            top.found[i] = k > none_key() ? k : (key_t)i;                          // (fillers: keys of their own, below all others)
-        }
+        if (tid < GROUPS) top.short_group[tid] = short_key((uint32_t)(first >> 32), tid);
+        if (tid == 0) top.count = 0;
         __syncthreads();
-        select_top(top, n, a.top);
+        const key_t least = max((key_t)short_rank(top, a.top) << 32, none_key() + 1);
+#pragma unroll
+        for (int i = 0; i < MOST; ++i)
+            if (mine[i] >= least) top.found[atomicAdd(&top.count, 1)] = mine[i];
+        __syncthreads();
+        select_top(top, top.count, a.top);
     }
-    finish_row<TYPE>(a, row, st, top.list);
+    finish_row<TYPE>(a, row, st, top.list, own);
 }
 
 struct LogprobGradArgs {
@@ -379,7 +479,7 @@ xnor_status launch_logprobs(const void *logits, long long stride, const void *to
                         stride, vocab, given, top, token_bytes, parts, logprobs_per_part(vocab, parts)};
     const dim3 grid((unsigned)(rows * parts)), threads(THREADS);
     by_type(type, [&](auto t) {
-        const size_t lds = top_lds(top, top * GROUP_LANES * 8 * STEPS);
+        const size_t lds = top_lds(top, 32 + top * GROUP_LANES * 8 * STEPS);
         if (top && entropy) logprobs_kernel<t(), true, true><<<grid, threads, lds, stream>>>(a);
         else if (top) logprobs_kernel<t(), true, false><<<grid, threads, lds, stream>>>(a);
         else if (entropy) logprobs_kernel<t(), false, true><<<grid, threads, 0, stream>>>(a);

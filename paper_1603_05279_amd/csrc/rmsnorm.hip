@@ -134,7 +134,9 @@ __global__ __launch_bounds__(1024) void rmsnorm_q8_kernel(NormArgs a)
                 typedef uint32_t words2 __attribute__((ext_vector_type(2), aligned(1)));
                 *reinterpret_cast<words2 *>(p) = words2{q.w[0], q.w[1]};
             } else {
-                for (int j = 0; j < n; ++j) p[j] = q.b[j];
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j < n) p[j] = q.b[j];
             }
         }
         if (a.values) values.store(static_cast<T *>(a.values) + row * a.cols + c, n);
@@ -169,18 +171,25 @@ __global__ __launch_bounds__(1024) void rmsnorm_grad_kernel(NormGradArgs a)
         const T *g = static_cast<const T *>(a.g) + (size_t)row * a.g_stride;
         const T *gs = static_cast<const T *>(a.g_sum) + (a.g_sum ? (size_t)row * a.g_sum_stride : 0);
         const float rstd = a.rstd[row];
+        constexpr bool HELD = STEPS < 4;                // (the longest rows are read twice: their registers hold the shares of g_weight)
         Real8<TYPE> hv[STEPS], gv[STEPS], sv[STEPS];
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
+        auto load = [&](int i) {
             const int c = 8 * (tid + i * (int)blockDim.x);
             hv[i].load(h + c, a.cols - c);
             gv[i].load(g + c, a.cols - c);
             if (a.g_sum) sv[i].load(gs + c, a.cols - c);
-        }
+        };
+        if (HELD)
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) load(i);
         float dot = 0.0f;
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
             const int c = 8 * (tid + i * (int)blockDim.x);
+            if (!HELD) {                                // (one step's values at a time, and none kept for the second time)
+                asm volatile("" : "+s"(h), "+s"(g), "+s"(gs) : : "memory");
+                load(i);
+            }
             Real8<XNOR_F32> w;
             if (a.weight) w.load(a.weight + c, a.cols - c);
 #pragma unroll
@@ -195,6 +204,10 @@ __global__ __launch_bounds__(1024) void rmsnorm_grad_kernel(NormGradArgs a)
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
             const int c = 8 * (tid + i * (int)blockDim.x);
+            if (!HELD) {                                // (one step's values at a time, and none kept for the second time)
+                asm volatile("" : "+s"(h), "+s"(g), "+s"(gs) : : "memory");
+                load(i);
+            }
             Real8<XNOR_F32> w;
             if (a.weight) w.load(a.weight + c, a.cols - c);
             Real8<TYPE> o;
@@ -226,6 +239,7 @@ __global__ __launch_bounds__(1024) void rmsnorm_grad_sum_kernel(const float *__r
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
     float s = 0.0f;
     if (c < cols)
+#pragma unroll 8
         for (int p = wave; p < parts; p += 16) s += partial[(size_t)p * cols + c];
     sums[wave][lane] = s;
     __syncthreads();
