@@ -21,11 +21,12 @@ xnor_status launch_w4_linear(const void *x, long long x_stride, const void *wimg
                              hipStream_t stream);
 xnor_status launch_w4_linear_q8(const int8_t *q, const float *x_scale, const void *wimg, void *y, void *workspace, int rows, int in, int out, int group,
                                 int x_group, int type, hipStream_t stream);
-// products of many rows (w4_tiles.hip); form: the rows' xnor_dtype, or 3 for 8 bits
-bool w4_tiles_applies(int rows);
-size_t w4_tiles_workspace_bytes(int rows, int in, int out, int group);
-xnor_status launch_w4_tiles(const void *x, long long x_stride, const float *x_scale, const void *wimg, void *y, void *workspace, int rows, int in, int out,
-                            int group, int x_group, int form, int type, hipStream_t stream);
+// products (form: the rows' xnor_dtype, or 3 for 8 bits): w4_rows_kernel, or the kernels of w4_tiles.hip on staged rows
+enum W4Kernel { W4_ROWS, W4_WAVES, W4_TILES };
+W4Kernel w4_kernel(int rows, int in, int out, int form);
+size_t w4_staged_bytes(int rows, int in, int out, int group);
+xnor_status launch_w4_staged(W4Kernel kernel, const void *x, long long x_stride, const float *x_scale, const void *wimg, void *y, void *workspace, int rows,
+                             int in, int out, int group, int x_group, int form, int type, hipStream_t stream);
 size_t logprobs_workspace_bytes(int rows, int vocab, int top);
 xnor_status launch_logprobs(const void *logits, long long stride, const void *tokens, int token_bytes, float *logprob, float *lse, float *shift, float *entropy,
                             int32_t *top_index, float *top_logprob, void *workspace, int rows, int vocab, int given, int top, int type,

@@ -30,11 +30,10 @@ template <int X> struct Form {          // 16 bits
     }
     static __device__ __forceinline__ operand_t widen(uint32_t w)
     {
-        if (X == ROWS_F16)
-            return operand_t{(w << 6 & 0x03c003c0u) | 0x4c004c00u, (w << 2 & 0x03c003c0u) | 0x4c004c00u, (w >> 2 & 0x03c003c0u) | 0x4c004c00u,
-                             (w >> 6 & 0x03c003c0u) | 0x4c004c00u};
-        return operand_t{(w << 3 & 0x00780078u) | 0x41804180u, (w >> 1 & 0x00780078u) | 0x41804180u, (w >> 5 & 0x00780078u) | 0x41804180u,
-                         (w >> 9 & 0x00780078u) | 0x41804180u};
+        uint32_t mask = X == ROWS_F16 ? 0x03c003c0u : 0x00780078u, base = X == ROWS_F16 ? 0x4c004c00u : 0x41804180u;
+        asm("" : "+v"(mask), "+v"(base));           // (in registers: an and-or takes no two literals)
+        if (X == ROWS_F16) return operand_t{(w << 6 & mask) | base, (w << 2 & mask) | base, (w >> 2 & mask) | base, (w >> 6 & mask) | base};
+        return operand_t{(w << 3 & mask) | base, (w >> 1 & mask) | base, (w >> 5 & mask) | base, (w >> 9 & mask) | base};
     }
     static __device__ __forceinline__ acc_t mfma(operand_t a, operand_t b, acc_t c)
     {
@@ -48,7 +47,12 @@ template <> struct Form<ROWS_I8> {
     typedef i32x4 acc_t;
     typedef long operand_t;             // bytes 0 4 1 5 2 6 3 7 of eight neighbours
     // z: the zero point in every byte
-    static __device__ __forceinline__ uint32_t minus(uint32_t u, uint32_t z) { return ((u & 0x0f0f0f0fu) | 0x80808080u) - z ^ 0x80808080u; }
+    static __device__ __forceinline__ uint32_t minus(uint32_t u, uint32_t z)
+    {
+        uint32_t mask = 0x0f0f0f0fu, top = 0x80808080u;
+        asm("" : "+v"(mask), "+v"(top));
+        return ((u & mask) | top) - z ^ top;
+    }
     static __device__ __forceinline__ operand_t widen(uint32_t w, uint32_t z)
     {
         return (operand_t)((uint64_t)minus(w, z) | (uint64_t)minus(w >> 4, z) << 32);
@@ -122,7 +126,9 @@ __device__ __forceinline__ void store_four(void *y, int type, size_t at, f32x4 v
         typedef float four __attribute__((ext_vector_type(4), aligned(4)));
         if (n >= 4) *reinterpret_cast<four *>(p) = v;
         else
-            for (int i = 0; i < n; ++i) p[i] = v[i];
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (i < n) p[i] = v[i];
         return;
     }
     typedef uint16_t halves __attribute__((ext_vector_type(4), aligned(2)));
@@ -133,7 +139,9 @@ __device__ __forceinline__ void store_four(void *y, int type, size_t at, f32x4 v
     uint16_t *p = static_cast<uint16_t *>(y) + at;
     if (n >= 4) *reinterpret_cast<halves *>(p) = h;
     else
-        for (int i = 0; i < n; ++i) p[i] = h[i];
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < n) p[i] = h[i];
 }
 
 }  // namespace xnor

@@ -89,114 +89,184 @@ struct W4Args {
     const uint8_t *image;
     void *y;
     long long x_stride;             // in elements
-    int rows, in, out, group, x_group, x_groups;
+    int rows, in, out, x_groups, x_shift, type;     // a group's scale of x: group >> x_shift
 };
 
-// A workgroup makes 16 outputs of 16 * BLOCKS rows; its waves take every WAVES-th chunk of 128 inputs and add their sums in LDS.  Nothing is
-// staged: a code is read once, straight from the image into the lane that multiplies it.
-template <int X, int YTYPE, int BLOCKS, int WAVES>
+// What a wave multiplies at a time: 16 * TILES outputs, 128 inputs, 16 * BLOCKS rows.
+template <int X, int BLOCKS, int TILES, int STEPS> struct Chunk {
+    static constexpr int GROUPS = 4 / STEPS;
+    u32x4 w[TILES];
+    Eight<X> x[4][BLOCKS];
+    f32x4 s[GROUPS][TILES];
+    uint32_t z[GROUPS][TILES];      // 16 bits: of a lane's four results; 8 bits: of its operand
+    float xs[X == ROWS_I8 ? GROUPS : 1][BLOCKS];
+};
+
+// A workgroup makes 16 * TILES outputs of 16 * BLOCKS rows; its waves take every WAVES-th chunk of 128 inputs and add their sums in LDS.  Nothing
+// is staged: a code is read once, straight from the image into the lane that multiplies it, DEPTH chunks ahead.  Lanes past the last row multiply
+// it once more.  GROUPED: 8-bit rows with scales of groups.
+template <int X, int BLOCKS, int TILES, int STEPS, bool GROUPED, int WAVES, int DEPTH>
 __global__ __launch_bounds__(64 * WAVES) void w4_rows_kernel(W4Args a)
 {
     typedef Form<X> F;
-    typedef real_t<YTYPE> Y;
-    __shared__ __attribute__((aligned(16))) float red[WAVES][16 * BLOCKS][20];
-    const W4Layout l(a.out, a.in, a.group);
+    typedef Chunk<X, BLOCKS, TILES, STEPS> C;
+    constexpr int GROUP = 32 * STEPS, XBYTES = X == ROWS_F32 ? 4 : X == ROWS_I8 ? 1 : 2, PITCH = 16 * TILES + 4;
+    __shared__ __attribute__((aligned(16))) float red[WAVES][16 * BLOCKS][PITCH];
+    const W4Layout l(a.out, a.in, GROUP);
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quarter = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int tile = blockIdx.x, row0 = blockIdx.y * 16 * BLOCKS;
-    const u32x4 *codes = reinterpret_cast<const u32x4 *>(a.image) + (size_t)tile * l.chunks * 64 + lane;
-    const float *scales = reinterpret_cast<const float *>(a.image + l.scale_at()) + (size_t)tile * l.groups * 16 + 4 * quarter;
-    const uint8_t *zeros = a.image + l.zero_at() + (size_t)tile * l.groups * 16 + (X == ROWS_I8 ? col : 4 * quarter);
+    const int tile0 = blockIdx.x * TILES, row0 = blockIdx.y * 16 * BLOCKS;
+    // (a workgroup's tiles past the last one multiply the last once more)
+    const u32x4 *codes[TILES];
+    const float *scales[TILES];
+    const uint8_t *zeros[TILES];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) {
+        const size_t tile = min(tile0 + t, l.tiles - 1);
+        codes[t] = reinterpret_cast<const u32x4 *>(a.image) + tile * l.chunks * 64 + lane;
+        scales[t] = reinterpret_cast<const float *>(a.image + l.scale_at()) + tile * l.groups * 16 + 4 * quarter;
+        zeros[t] = a.image + l.zero_at() + tile * l.groups * 16 + (X == ROWS_I8 ? col : 4 * quarter);
+    }
     const char *xrow[BLOCKS];
-    bool real[BLOCKS];
-    constexpr int XBYTES = X == ROWS_F32 ? 4 : X == ROWS_I8 ? 1 : 2;
+    const float *xscale[BLOCKS];
 #pragma unroll
     for (int b = 0; b < BLOCKS; ++b) {
-        const int row = row0 + 16 * b + col;
-        real[b] = row < a.rows;
-        xrow[b] = static_cast<const char *>(a.x) + (size_t)(real[b] ? row : 0) * a.x_stride * XBYTES;
+        const size_t row = min(row0 + 16 * b + col, a.rows - 1);
+        xrow[b] = static_cast<const char *>(a.x) + row * a.x_stride * XBYTES;
+        xscale[b] = a.x_scale + row * a.x_groups;
     }
-    f32x4 total[BLOCKS];
+    f32x4 total[TILES][BLOCKS];
 #pragma unroll
-    for (int b = 0; b < BLOCKS; ++b) total[b] = f32x4{0, 0, 0, 0};
-    const int steps_per_group = a.group / 32;
-    for (int chunk = wave; chunk < l.chunks; chunk += WAVES) {
-        const u32x4 w = codes[(size_t)chunk * 64];
-        Eight<X> x[4][BLOCKS];
+    for (int t = 0; t < TILES; ++t)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int b = 0; b < BLOCKS; ++b) total[t][b] = f32x4{0, 0, 0, 0};
+    // whole: 128 inputs exist.  A group past the last input has sums of zero, whatever it is scaled with
+    auto load = [&](C &c, int chunk, bool whole) {
 #pragma unroll
-            for (int b = 0; b < BLOCKS; ++b) {
-                const int k = 128 * chunk + 32 * j + 8 * quarter;
-                x[j][b].load(xrow[b], k, real[b] ? a.in - k : 0);
-            }
-        typename F::acc_t acc[BLOCKS], sum[BLOCKS];
-        uint32_t zero = 0;
+        for (int t = 0; t < TILES; ++t) c.w[t] = codes[t][(size_t)chunk * 64];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int k0 = 128 * chunk + 32 * j, g = min(k0 / a.group, l.groups - 1);
-            if (j % steps_per_group == 0) {
+            const int k = 128 * chunk + 32 * j + 8 * quarter;
 #pragma unroll
-                for (int b = 0; b < BLOCKS; ++b) acc[b] = sum[b] = typename F::acc_t{0, 0, 0, 0};
-                if (X == ROWS_I8) zero = zeros[(size_t)g * 16] * 0x01010101u;
+            for (int b = 0; b < BLOCKS; ++b) c.x[j][b].load(xrow[b], k, whole ? 8 : a.in - k);
+        }
+#pragma unroll
+        for (int i = 0; i < C::GROUPS; ++i) {
+            const int g = whole ? chunk * C::GROUPS + i : min(chunk * C::GROUPS + i, l.groups - 1);
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                c.s[i][t] = *reinterpret_cast<const f32x4 *>(scales[t] + (size_t)g * 16);
+                c.z[i][t] = X == ROWS_I8 ? zeros[t][(size_t)g * 16] : *reinterpret_cast<const uint32_t *>(zeros[t] + (size_t)g * 16);
+            }
+            if (GROUPED)
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b) c.xs[i][b] = xscale[b][g >> a.x_shift];
+        }
+    };
+    auto multiply = [&](const C &c) {
+        typename F::acc_t acc[TILES][BLOCKS], sum[BLOCKS];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (j % STEPS == 0)
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b) {
+                    sum[b] = typename F::acc_t{0, 0, 0, 0};
+#pragma unroll
+                    for (int t = 0; t < TILES; ++t) acc[t][b] = typename F::acc_t{0, 0, 0, 0};
+                }
+            typename F::operand_t wide[TILES];
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                if constexpr (X == ROWS_I8) wide[t] = F::widen(c.w[t][j], c.z[j / STEPS][t] * 0x01010101u);
+                else wide[t] = F::widen(c.w[t][j]);
             }
 #pragma unroll
             for (int b = 0; b < BLOCKS; ++b) {
                 typename F::operand_t xo[F::PARTS];
-                x[j][b].operands(xo);
-                if constexpr (X == ROWS_I8) {
-                    acc[b] = F::mfma(F::widen(w[j], zero), xo[0], acc[b]);
-                } else {
+                c.x[j][b].operands(xo);
 #pragma unroll
-                    for (int p = 0; p < F::PARTS; ++p) {
-                        acc[b] = F::mfma(F::widen(w[j]), xo[p], acc[b]);
-                        sum[b] = F::mfma(F::ones(), xo[p], sum[b]);
-                    }
+                for (int p = 0; p < F::PARTS; ++p) {
+#pragma unroll
+                    for (int t = 0; t < TILES; ++t) acc[t][b] = F::mfma(wide[t], xo[p], acc[t][b]);
+                    if constexpr (X != ROWS_I8) sum[b] = F::mfma(F::ones(), xo[p], sum[b]);
                 }
             }
-            if ((j + 1) % steps_per_group == 0) {           // (a group past the last input has sums of zero)
-                const f32x4 s = *reinterpret_cast<const f32x4 *>(scales + (size_t)g * 16);
-                uint32_t z = 0;
-                if constexpr (X != ROWS_I8) z = *reinterpret_cast<const uint32_t *>(zeros + (size_t)g * 16);
+            if (j % STEPS != STEPS - 1) continue;
 #pragma unroll
-                for (int b = 0; b < BLOCKS; ++b) {
-                    float xs = 1.0f;
-                    if (X == ROWS_I8 && a.x_group)
-                        xs = a.x_scale[(size_t)min(row0 + 16 * b + col, a.rows - 1) * a.x_groups + min(k0 / a.x_group, a.x_groups - 1)];
+            for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
                     for (int v = 0; v < 4; ++v) {
                         float part;
-                        if constexpr (X == ROWS_I8) part = (float)acc[b][v] * xs;
-                        else part = __builtin_fmaf(-(F::OFFSET + (float)(z >> (8 * v) & 255u)), sum[b][v], acc[b][v]);
-                        total[b][v] = __builtin_fmaf(s[v], part, total[b][v]);
+                        if constexpr (X == ROWS_I8) part = GROUPED ? (float)acc[t][b][v] * c.xs[j / STEPS][b] : (float)acc[t][b][v];
+                        else part = __builtin_fmaf(-(F::OFFSET + (float)(c.z[j / STEPS][t] >> (8 * v) & 255u)), sum[b][v], acc[t][b][v]);
+                        total[t][b][v] = __builtin_fmaf(c.s[j / STEPS][t][v], part, total[t][b][v]);
                     }
-                }
-            }
+        }
+    };
+    const int whole = a.in / 128;
+    C ring[DEPTH];
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d)
+        if (wave + d * WAVES < whole) load(ring[d], wave + d * WAVES, true);
+    for (int chunk = wave; chunk < whole; chunk += DEPTH * WAVES) {
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            if (chunk + d * WAVES >= whole) break;
+            multiply(ring[d]);
+            if (chunk + (d + DEPTH) * WAVES < whole) load(ring[d], chunk + (d + DEPTH) * WAVES, true);
         }
     }
+    if (whole < l.chunks && wave == whole % WAVES) {        // the inputs past the last whole chunk
+        load(ring[0], whole, false);
+        multiply(ring[0]);
+    }
 #pragma unroll
-    for (int b = 0; b < BLOCKS; ++b) *reinterpret_cast<f32x4 *>(&red[wave][16 * b + col][4 * quarter]) = total[b];
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) *reinterpret_cast<f32x4 *>(&red[wave][16 * b + col][16 * t + 4 * quarter]) = total[t][b];
     __syncthreads();
-    for (int i = tid; i < 64 * BLOCKS; i += 64 * WAVES) {
-        const int r = i >> 2, q = i & 3, row = row0 + r, o = 16 * tile + 4 * q;
+    for (int i = tid; i < 64 * BLOCKS * TILES; i += 64 * WAVES) {
+        const int r = i / (4 * TILES), q = i % (4 * TILES), row = row0 + r, o = 16 * tile0 + 4 * q;
+        if (row >= a.rows) continue;
         f32x4 s = *reinterpret_cast<const f32x4 *>(&red[0][r][4 * q]);
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) s += *reinterpret_cast<const f32x4 *>(&red[w][r][4 * q]);
-        if (row >= a.rows) continue;
-        if (X == ROWS_I8 && !a.x_group) s *= a.x_scale[row];
-        Y *y = static_cast<Y *>(a.y) + (size_t)row * a.out + o;
-#pragma unroll
-        for (int v = 0; v < 4; ++v)
-            if (o + v < a.out) y[v] = (Y)s[v];
+        if (X == ROWS_I8 && !GROUPED) s *= a.x_scale[row];
+        store_four(a.y, a.type, (size_t)row * a.out + o, s, a.out - o);
     }
 }
 
-template <int X, int YTYPE> void launch_rows(const W4Args &a, hipStream_t stream)
+template <int X, bool GROUPED, int STEPS, int BLOCKS, int TILES, int DEPTH> void launch_rows(const W4Args &a, hipStream_t stream)
 {
-    const unsigned tiles = (unsigned)((a.out + 15) / 16);
-    if (a.rows <= 16) w4_rows_kernel<X, YTYPE, 1, 8><<<dim3(tiles, 1), dim3(512), 0, stream>>>(a);
-    else if (a.rows <= 32) w4_rows_kernel<X, YTYPE, 2, 8><<<dim3(tiles, 1), dim3(512), 0, stream>>>(a);
-    else w4_rows_kernel<X, YTYPE, 4, 8><<<dim3(tiles, (unsigned)((a.rows + 63) / 64)), dim3(512), 0, stream>>>(a);
+    const dim3 grid((unsigned)((a.out + 16 * TILES - 1) / (16 * TILES)), (unsigned)((a.rows + 16 * BLOCKS - 1) / (16 * BLOCKS)));
+    w4_rows_kernel<X, BLOCKS, TILES, STEPS, GROUPED, 8, DEPTH><<<grid, dim3(512), 0, stream>>>(a);
+}
+// Tiles of outputs per workgroup and chunks ahead.  More tiles read the rows' inputs less often, and leave fewer workgroups: they pay where those still fill
+// the chip.  8 8-bit rows 4096 -> 32000 (2000 tiles): one tile 24 us, two 16.0, four 13.4; 16 bfloat16 rows 4096 -> 16384: four 10.7, two 13.7; one row
+// 9216 -> 4096 (256 tiles): one 7.2, two 10.2, four 18.  (Sixteen waves 6.9 on the last, 30 on the first; four chunks ahead of a tile 7.2 and 25.5.)
+template <int X, bool GROUPED, int STEPS> void launch_steps(const W4Args &a, hipStream_t stream)
+{
+    constexpr int TWO = X == ROWS_F32 ? 1 : 2;          // (float32 rows fill the registers)
+    const int tiles = (a.out + 15) / 16;
+    if (a.rows <= 16) {
+        if (tiles >= 1024) launch_rows<X, GROUPED, STEPS, 1, 4, 1>(a, stream);
+        else if (tiles >= 512) launch_rows<X, GROUPED, STEPS, 1, 2, TWO>(a, stream);
+        else launch_rows<X, GROUPED, STEPS, 1, 1, TWO>(a, stream);
+    } else if (a.rows <= 32) {
+        if (tiles >= 512) launch_rows<X, GROUPED, STEPS, 2, 2, 1>(a, stream);
+        else launch_rows<X, GROUPED, STEPS, 2, 1, TWO>(a, stream);
+    } else {
+        launch_rows<X, GROUPED, STEPS, 4, 1, 1>(a, stream);
+    }
+}
+template <int X, bool GROUPED> xnor_status launch_groups(const W4Args &a, int group, hipStream_t stream)
+{
+    if (group == 32) launch_steps<X, GROUPED, 1>(a, stream);
+    else if (group == 64) launch_steps<X, GROUPED, 2>(a, stream);
+    else launch_steps<X, GROUPED, 4>(a, stream);
+    return hip_status(hipGetLastError());
 }
 
 }  // namespace
@@ -223,27 +293,27 @@ xnor_status launch_w4_pack(const uint8_t *codes, const float *scale, const uint8
     return hip_status(hipGetLastError());
 }
 
-size_t w4_linear_workspace_bytes(int rows, int in, int out, int group)
-{
-    return w4_tiles_applies(rows) ? w4_tiles_workspace_bytes(rows, in, out, group) : 0;
-}
+size_t w4_linear_workspace_bytes(int rows, int in, int out, int group) { return w4_staged_bytes(rows, in, out, group); }
 
 xnor_status launch_w4_linear(const void *x, long long x_stride, const void *wimg, void *y, void *workspace, int rows, int in, int out, int group, int type,
                              hipStream_t stream)
 {
-    if (w4_tiles_applies(rows)) return launch_w4_tiles(x, x_stride, nullptr, wimg, y, workspace, rows, in, out, group, 0, type, type, stream);
-    const W4Args a{x, nullptr, static_cast<const uint8_t *>(wimg), y, x_stride, rows, in, out, group, 0, 1};
-    by_type(type, [&](auto t) { launch_rows<t(), t()>(a, stream); });
-    return hip_status(hipGetLastError());
+    const W4Kernel kernel = w4_kernel(rows, in, out, type);
+    if (kernel != W4_ROWS) return launch_w4_staged(kernel, x, x_stride, nullptr, wimg, y, workspace, rows, in, out, group, 0, type, type, stream);
+    const W4Args a{x, nullptr, static_cast<const uint8_t *>(wimg), y, x_stride, rows, in, out, 0, 0, type};
+    if (type == XNOR_F32) return launch_groups<ROWS_F32, false>(a, group, stream);
+    if (type == XNOR_BF16) return launch_groups<ROWS_BF16, false>(a, group, stream);
+    return launch_groups<ROWS_F16, false>(a, group, stream);
 }
 
 xnor_status launch_w4_linear_q8(const int8_t *q, const float *x_scale, const void *wimg, void *y, void *workspace, int rows, int in, int out, int group,
                                 int x_group, int type, hipStream_t stream)
 {
-    if (w4_tiles_applies(rows)) return launch_w4_tiles(q, in, x_scale, wimg, y, workspace, rows, in, out, group, x_group, ROWS_I8, type, stream);
-    const W4Args a{q, x_scale, static_cast<const uint8_t *>(wimg), y, in, rows, in, out, group, x_group, x_group ? (in + x_group - 1) / x_group : 1};
-    by_type(type, [&](auto t) { launch_rows<ROWS_I8, t()>(a, stream); });
-    return hip_status(hipGetLastError());
+    const W4Kernel kernel = w4_kernel(rows, in, out, ROWS_I8);
+    if (kernel != W4_ROWS) return launch_w4_staged(kernel, q, in, x_scale, wimg, y, workspace, rows, in, out, group, x_group, ROWS_I8, type, stream);
+    const W4Args a{q, x_scale, static_cast<const uint8_t *>(wimg), y, in, rows, in, out, x_group ? (in + x_group - 1) / x_group : 0,
+                   x_group ? __builtin_ctz(x_group / group) : 0, type};
+    return x_group ? launch_groups<ROWS_I8, true>(a, group, stream) : launch_groups<ROWS_I8, false>(a, group, stream);
 }
 
 }  // namespace xnor

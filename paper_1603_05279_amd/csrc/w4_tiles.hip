@@ -4,13 +4,13 @@
 #include "w4_form.h"
 #include "w4_image.h"
 #include <algorithm>
+#include <cmath>
 
 namespace xnor {
 
 namespace {
 
 constexpr int TILE = 16, BLOCK = 8;         // rows or outputs of a matrix instruction, such tiles of a workgroup's side
-constexpr int SPLIT_CHUNKS = 4;             // a share of the inputs is a multiple of 4 chunks: whole quads of groups
 
 // What the rows become (the first kernel writes it, the second reads it), in a workspace of the caller's:
 //   operands  [block of 128 rows][chunk of 128 inputs][part][tile of 16 rows][step][lane][16 bytes]: 16 bits, 4 steps of 32 inputs; 8 bits, 2 steps
@@ -18,7 +18,6 @@ constexpr int SPLIT_CHUNKS = 4;             // a share of the inputs is a multip
 //   sums      [tile of 16 rows][quad of groups][lane][16 bytes], 16 bits only: the groups' sums of x as three bfloat16 numbers in an order that
 //             gives all products with a second factor's three but the smallest: lane 16 i + r is row r, group i of the quad
 //   scales    [tile of 16 rows][group][row] float32, 8-bit rows with scales of groups only
-//   partial   [share][row][out, whole tiles] float32, where the inputs are shared out
 struct Staged {
     int blocks, chunks, parts, groups, quads;
     bool bytes;
@@ -28,7 +27,7 @@ struct Staged {
     __host__ __device__ int tile_bytes() const { return bytes ? 2048 : 4096; }
     __host__ __device__ size_t sums_at() const { return (size_t)blocks * chunks * parts * BLOCK * tile_bytes(); }
     __host__ __device__ size_t scales_at() const { return sums_at() + (size_t)blocks * BLOCK * quads * 1024; }
-    __host__ __device__ size_t partial_at() const { return scales_at() + (bytes ? (size_t)blocks * BLOCK * groups * 64 : 0); }
+    __host__ __device__ size_t total() const { return scales_at() + (bytes ? (size_t)blocks * BLOCK * groups * 64 : 0); }
 };
 
 // x cut off to three bfloat16 numbers whose sum it is (an infinity has no rest)
@@ -39,6 +38,14 @@ __device__ __forceinline__ void three_parts(float x, uint32_t *p)
     const float rest = finite ? x - __uint_as_float(p[0] << 16) : 0.0f;
     p[1] = __float_as_uint(rest) >> 16;
     p[2] = __float_as_uint(rest - __uint_as_float(p[1] << 16)) >> 16;
+}
+
+// - scale (OFFSET + zero) as three bfloat16 numbers in the order that meets those of a group's sum
+template <int X> __device__ __forceinline__ bf16x8 offset_parts(float scale, uint8_t zero)
+{
+    uint32_t p[3];
+    three_parts(-(scale * (Form<X>::OFFSET + (float)zero)), p);
+    return __builtin_bit_cast(bf16x8, u32x4{p[0] | p[0] << 16, p[1] | p[1] << 16, p[0] | p[2] << 16, p[1] | p[2] << 16});
 }
 
 struct StageArgs {
@@ -119,10 +126,9 @@ __global__ __launch_bounds__(256) void w4_stage_kernel(StageArgs a)
 struct TileArgs {
     const uint8_t *staged, *image;
     const float *x_scale;
-    float *partial;
     void *y;
-    int rows, in, out, group, type, form;
-    int row_blocks, out_blocks, shares, per_share;      // chunks of a share
+    int rows, in, out, type, form;
+    int row_blocks, out_blocks;
 };
 
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
@@ -133,168 +139,189 @@ __device__ __forceinline__ void to_lds(const uint8_t *from, uint8_t *to)        
     __builtin_amdgcn_global_load_lds((global_u8 *)from, (lds_u8 *)to, 16, 0, 0);
 }
 
-// STEPS of 32 inputs per group.  Four waves, each 64 outputs x 64 rows.  The rows' operands of a chunk and the weights' scales go straight to LDS while the
-// chunk before is multiplied (two buffers, one barrier per chunk); the codes go to the registers of the lanes that multiply them.
-// GROUPED: 8-bit rows with scales of groups.
-template <int X, int STEPS, bool GROUPED>
-__global__ __launch_bounds__(256, 2) void w4_tiles_kernel(TileArgs a)
+// STEPS of 32 inputs per group.  2 * SIDE waves, each 64 outputs x 64 rows, together 64 * SIDE outputs x 128 rows.  All a chunk needs (the rows' operands,
+// codes, scales, zero points) goes straight to one of BUFFERS places in LDS, BUFFERS - 1 chunks ahead, one barrier per chunk.  Every wave issues
+// the same number of loads for a chunk, so that it can wait for its oldest chunk alone.  GROUPED: 8-bit rows with scales of groups.
+template <int X, int STEPS, bool GROUPED, int SIDE> struct TilePlace {
+    static constexpr int WAVES = 2 * SIDE, PER_CHUNK = 4 / STEPS, TB = X == ROWS_I8 ? 2048 : 4096;
+    static constexpr int ROWS = 0, CODES = BLOCK * TB, SCALES = CODES + SIDE * 4096, FACTORS = 4 * PER_CHUNK * 64;      // of four tiles
+    static constexpr int ROW_SCALES = SCALES + SIDE * FACTORS, ZEROS = ROW_SCALES + (GROUPED ? 2 * FACTORS : 0);
+    static constexpr int BYTES = ZEROS + (X == ROWS_I8 ? SIDE * FACTORS / 4 : 0);
+    static constexpr int LOADS = BLOCK * TB / (WAVES * 1024) + 2 + 1 + (GROUPED ? 1 : 0) + (X == ROWS_I8 ? 1 : 0);
+};
+
+template <int X, int STEPS, bool GROUPED, int SIDE, int BUFFERS>
+__global__ __launch_bounds__(128 * SIDE) void w4_tiles_kernel(TileArgs a)
 {
     typedef Form<X> F;
-    constexpr int TB = X == ROWS_I8 ? 2048 : 4096, PER_CHUNK = 4 / STEPS;
-    constexpr int FACTORS = BLOCK * PER_CHUNK * 64;                              // bytes of the scales of a chunk
-    constexpr int ZEROS = X == ROWS_I8 ? BLOCK * PER_CHUNK * 16 : 0;              // and of the zero points, where the sums are exact
-    constexpr int BUFFER = BLOCK * TB + FACTORS * (GROUPED ? 2 : 1) + ZEROS;
+    typedef TilePlace<X, STEPS, GROUPED, SIDE> P;
+    constexpr int WAVES = P::WAVES, AHEAD = BUFFERS - 1, TB = P::TB, PER_CHUNK = P::PER_CHUNK;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    const W4Layout l(a.out, a.in, a.group);
-    const Staged st(a.rows, a.in, a.group, a.form);
+    const W4Layout l(a.out, a.in, 32 * STEPS);
+    const Staged st(a.rows, a.in, 32 * STEPS, a.form);
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quarter = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wo = wave & 1, wr = wave >> 1;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wo = wave % SIDE, wr = wave / SIDE;
     // workgroups go to the XCDs in turn: each takes a run of neighbouring tiles
-    const int count = a.row_blocks * a.out_blocks * a.shares, per_xcd = (count + 7) / 8;
+    const int count = a.row_blocks * a.out_blocks, per_xcd = (count + 7) / 8;
     const int id = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
     if ((int)(blockIdx.x >> 3) >= per_xcd || id >= count) return;
-    const int share = id / (a.row_blocks * a.out_blocks), rest = id % (a.row_blocks * a.out_blocks);
-    const int rb = rest % a.row_blocks, ob = rest / a.row_blocks;
-    const int otile = ob * BLOCK + wo * 4, rtile = rb * BLOCK + wr * 4;
-    const int first = share * a.per_share, last = min(first + a.per_share, l.chunks);
-    const int parts = st.parts;
+    const int rb = id % a.row_blocks, ob = id / a.row_blocks;
+    const int otile = ob * 4 * SIDE + wo * 4, rtile = rb * BLOCK + wr * 4;
+    const int parts = st.parts, steps = st.chunks * parts;
 
-    const u32x4 *codes[4];
+    // (tiles past the last are the last once more)
+    const uint8_t *scales = a.image + l.scale_at(), *zeros = a.image + l.zero_at();
+    const uint8_t *rows_from = a.staged + (size_t)rb * steps * BLOCK * TB;
+    const uint8_t *codes_from[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) codes[i] = reinterpret_cast<const u32x4 *>(a.image) + (size_t)min(otile + i, l.tiles - 1) * l.chunks * 64 + lane;
-    const uint8_t *scales = a.image + l.scale_at();
-    const uint8_t *rows_from = a.staged + (size_t)rb * st.chunks * parts * BLOCK * TB;
-    // chunk c (parts of it one after another: step = chunk * parts + part)
-    auto fetch_rows = [&](int step, int buffer) {
-        const uint8_t *from = rows_from + (size_t)step * BLOCK * TB + tid * 16;
-        uint8_t *to = lds + buffer * BUFFER + wave * 1024;
+    for (int i = 0; i < 2; ++i) codes_from[i] = a.image + (size_t)min(ob * 4 * SIDE + wave * 2 + i, l.tiles - 1) * l.chunks * 1024;
+    // scales and zero points of a wave's four tiles: it loads a half of them, the wave of the other rows the other; the rows' scales: a share of each
+    // wave with the same rows.  Lanes: tile, group of the chunk, quarter of 16 factors (a lane per 16 bytes)
+    constexpr int SCALE_LANES = P::FACTORS / 32, ROW_LANES = P::FACTORS / 16 / SIDE, ZERO_LANES = P::FACTORS / 128;
+    const int otile0 = min(otile, l.tiles - 1), more = l.tiles - 1 - otile0;
+    const int f = min(lane, SCALE_LANES - 1) + wr * SCALE_LANES, fr = min(lane, ROW_LANES - 1) + wo * ROW_LANES, fz = min(lane, ZERO_LANES - 1) + wr * ZERO_LANES;
+    const uint8_t *scales_from = scales + (size_t)otile0 * l.groups * 64, *zeros_from = zeros + (size_t)otile0 * l.groups * 16;
+    const uint8_t *row_scales_from = a.staged + st.scales_at() + (size_t)rtile * l.groups * 64;
+    const uint32_t scale_off = (uint32_t)min(f / (4 * PER_CHUNK), more) * l.groups * 64 + (f & 3) * 16;
+    const uint32_t row_off = (uint32_t)(fr / (4 * PER_CHUNK)) * l.groups * 64 + (fr & 3) * 16;
+    const uint32_t zero_off = (uint32_t)min(fz / PER_CHUNK, more) * l.groups * 16;
+    const uint32_t at = tid * 16, lane_at = lane * 16;
+    // step = chunk * parts + part; a group past the last meets sums of zero
+    auto fetch = [&](int step, int place) {
+        const int c = parts == 1 ? step : (int)(__umulhi((uint32_t)step, 0xaaaaaaabu) >> 1), g0 = c * PER_CHUNK;
+        uint8_t *to = lds + place * P::BYTES;
+        const uint8_t *from = rows_from + (size_t)step * BLOCK * TB;
 #pragma unroll
-        for (int i = 0; i < BLOCK * TB / 4096; ++i) to_lds(from + i * 4096, to + i * 4096);
-        // scales: lane = tile, group of the chunk, quarter; a group past the last meets sums of zero
-        const int chunk = step / parts;
-        if (X == ROWS_I8 && wave == 3 && lane < BLOCK * PER_CHUNK) {
-            const int g = min(chunk * PER_CHUNK + lane % PER_CHUNK, l.groups - 1);
-            to_lds(a.image + l.zero_at() + ((size_t)min(ob * BLOCK + lane / PER_CHUNK, l.tiles - 1) * l.groups + g) * 16, lds + buffer * BUFFER + BUFFER - ZEROS);
-        }
-        if (wave * 64 < BLOCK * PER_CHUNK * 4) {
-            const int f = tid, tile = f / (PER_CHUNK * 4), g = min(chunk * PER_CHUNK + f / 4 % PER_CHUNK, l.groups - 1);
-            if (f < BLOCK * PER_CHUNK * 4) {
-                const size_t o = ((size_t)min(ob * BLOCK + tile, l.tiles - 1) * l.groups + g) * 64 + (f & 3) * 16;
-                to_lds(scales + o, lds + buffer * BUFFER + BLOCK * TB + wave * 1024);
-            }
-            if (GROUPED && f < BLOCK * PER_CHUNK * 4) {
-                const size_t o = ((size_t)(rb * BLOCK + tile) * l.groups + g) * 64 + (f & 3) * 16;
-                to_lds(a.staged + st.scales_at() + o, lds + buffer * BUFFER + BLOCK * TB + FACTORS + wave * 1024);
-            }
-        }
+        for (int i = 0; i < BLOCK * TB / (WAVES * 1024); ++i) to_lds(from + i * WAVES * 1024 + at, to + (i * WAVES + wave) * 1024);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) to_lds(codes_from[i] + (size_t)c * 1024 + lane_at, to + P::CODES + (wave * 2 + i) * 1024);
+        if (lane < SCALE_LANES)
+            to_lds(scales_from + (scale_off + (uint32_t)min(g0 + f / 4 % PER_CHUNK, l.groups - 1) * 64), to + P::SCALES + wo * P::FACTORS + wr * SCALE_LANES * 16);
+        if (GROUPED && lane < ROW_LANES)
+            to_lds(row_scales_from + (row_off + (uint32_t)min(g0 + fr / 4 % PER_CHUNK, l.groups - 1) * 64),
+                   to + P::ROW_SCALES + wr * P::FACTORS + wo * ROW_LANES * 16);
+        if (X == ROWS_I8 && lane < ZERO_LANES)
+            to_lds(zeros_from + (zero_off + (uint32_t)min(g0 + fz % PER_CHUNK, l.groups - 1) * 16), to + P::ZEROS + wo * P::FACTORS / 4 + wr * ZERO_LANES * 16);
     };
     f32x4 total[4][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) total[i][j] = f32x4{0, 0, 0, 0};
-    u32x4 w[4], next[4];
-    const int steps = (last - first) * parts;
-    fetch_rows(first * parts, 0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) next[i] = codes[i][(size_t)first * 64];
-    for (int s = 0; s < steps; ++s) {
-        const int buffer = s & 1;
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();                            // (the buffer is filled, the other one is read no more)
+    for (int r = 0; r < AHEAD; ++r) fetch(min(r, steps - 1), r);
+    // what the offset and the zero points add is taken out first, while the first chunks arrive: - scale (OFFSET + zero) times the groups' sums, four
+    // groups per instruction, both factors as three bfloat16 numbers (all products but the smallest: 2^-32 of the largest)
+    if constexpr (X != ROWS_I8) {
+        const u32x4 *sums = reinterpret_cast<const u32x4 *>(a.staged + st.sums_at()) + (size_t)rtile * st.quads * 64 + lane;
+        for (int quad = 0; quad < st.quads; ++quad) {
+            bf16x8 b[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = next[i];
-        if (s + 1 < steps) {
-            fetch_rows(first * parts + s + 1, buffer ^ 1);
-            const int chunk = first + (s + 1) / parts;
+            for (int j = 0; j < 4; ++j) b[j] = __builtin_bit_cast(bf16x8, sums[((size_t)j * st.quads + quad) * 64]);
+            const int g = min(4 * quad + quarter, l.groups - 1);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) next[i] = codes[i][(size_t)chunk * 64];
-        }
-        const uint8_t *x = lds + buffer * BUFFER + wr * 4 * TB + lane * 16;
-        const uint8_t *sw = lds + buffer * BUFFER + BLOCK * TB + wo * 4 * PER_CHUNK * 64 + quarter * 16;
-        const uint8_t *sx = lds + buffer * BUFFER + BLOCK * TB + FACTORS + wr * 4 * PER_CHUNK * 64 + col * 4;
-        const uint8_t *zero = lds + buffer * BUFFER + BUFFER - ZEROS + wo * 4 * PER_CHUNK * 16 + col;
-        // one tile of outputs after the other, so that the scaling of one meets the products of the next
-        constexpr int LOADS = TB / 1024;
-        u32x4 b[LOADS][4];
+            for (int i = 0; i < 4; ++i) {
+                const size_t f = ((size_t)min(otile + i, l.tiles - 1) * l.groups + g) * 16 + col;
+                const bf16x8 k = offset_parts<X>(reinterpret_cast<const float *>(scales)[f], zeros[f]);
 #pragma unroll
-        for (int t = 0; t < LOADS; ++t)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) b[t][j] = *reinterpret_cast<const u32x4 *>(x + j * TB + t * 1024);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            typename F::acc_t acc[4];
-            uint32_t z = 0;
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                if (t % STEPS == 0) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[j] = typename F::acc_t{0, 0, 0, 0};
-                    if (X == ROWS_I8) z = zero[(i * PER_CHUNK + t / STEPS) * 16] * 0x01010101u;
-                }
-                if constexpr (X != ROWS_I8) {
-                    const auto wide = F::widen(w[i][t]);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[j] = F::mfma(wide, b[t][j], acc[j]);
-                } else if constexpr (STEPS == 1) {          // (two groups in the 64 inputs of an instruction)
-                    const long wide = F::widen(w[i][t], z);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        acc[j] = F::mfma(wide, (long)((uint64_t)b[t / 2][j][2 * (t & 1)] | (uint64_t)b[t / 2][j][2 * (t & 1) + 1] << 32), acc[j]);
-                } else if (t % 2 == 0) {
-                    const uint32_t c0 = w[i][t], c1 = w[i][t + 1];
-                    const i32x4 wide{(int)F::minus(c0, z), (int)F::minus(c0 >> 4, z), (int)F::minus(c1, z), (int)F::minus(c1 >> 4, z)};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wide, __builtin_bit_cast(i32x4, b[t / 2][j]), acc[j], 0, 0, 0);
-                }
-                if (t % STEPS != STEPS - 1) continue;
-                const int g = t / STEPS;
-                const f32x4 f = *reinterpret_cast<const f32x4 *>(sw + (i * PER_CHUNK + g) * 64);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float c = GROUPED ? *reinterpret_cast<const float *>(sx + (j * PER_CHUNK + g) * 64) : 1.0f;
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) {
-                        float part = (float)acc[j][v];
-                        if (GROUPED) part *= c;
-                        total[i][j][v] = __builtin_fmaf(f[v], part, total[i][j][v]);
-                    }
-                }
+                for (int j = 0; j < 4; ++j) total[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, b[j], total[i][j], 0, 0, 0);
             }
         }
     }
-    // what the offset and the zero points add is taken out: - scale (OFFSET + zero) times the groups' sums, four groups per instruction, both
-    // factors as three bfloat16 numbers (all products but the smallest: 2^-32 of the largest)
-    const uint8_t *zeros = a.image + l.zero_at();
-    const int quad_end = min((last * PER_CHUNK + 3) / 4, st.quads);         // (none for 8 bits)
-    for (int quad = first * PER_CHUNK / 4; quad < quad_end; ++quad) {
-        bf16x8 b[4];
+    // A group's sums wait in acc, with the factors they are scaled by, until the first product of the next group takes their place: the scaling
+    // fills the time that the next chunk's operands take from LDS, and that a product takes.
+    constexpr int WIDE = X == ROWS_I8 && STEPS >= 2 ? 2 : 1, PHASES = 4 / WIDE;        // steps of 32 inputs per product, products per chunk
+    typename F::acc_t acc[4][4];
+    f32x4 factor[4];
+    float row_factor[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        factor[i] = f32x4{0, 0, 0, 0};
+        row_factor[i] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = typename F::acc_t{0, 0, 0, 0};
+    }
+    auto rescale = [&](int i) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            b[j] = __builtin_bit_cast(bf16x8, reinterpret_cast<const u32x4 *>(a.staged + st.sums_at())[((size_t)(rtile + j) * st.quads + quad) * 64 + lane]);
-        const int g = min(4 * quad + quarter, l.groups - 1);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const size_t f = ((size_t)min(otile + i, l.tiles - 1) * l.groups + g) * 16 + col;
-            uint32_t p[3];
-            three_parts(-(reinterpret_cast<const float *>(scales)[f] * (16.0f + (float)zeros[f])), p);
-            const u32x4 k{p[0] | p[0] << 16, p[1] | p[1] << 16, p[0] | p[2] << 16, p[1] | p[2] << 16};
+            for (int v = 0; v < 4; ++v) {
+                float part = (float)acc[i][j][v];
+                if (GROUPED) part *= row_factor[j];
+                total[i][j][v] = __builtin_fmaf(factor[i][v], part, total[i][j][v]);
+            }
+    };
+    int place = 0;
+    for (int s = 0; s < steps; ++s) {
+        // this chunk's loads are over (LOADS of each later one may not be), everybody's; and nobody reads the place of the chunk before
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((AHEAD - 1) * P::LOADS) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        const uint8_t *here = lds + place * P::BYTES, *x = here + wr * 4 * TB + lane_at, *wc = here + P::CODES + wo * 4096 + lane_at;
+        const uint8_t *sw = here + P::SCALES + wo * P::FACTORS + quarter * 16, *sx = here + P::ROW_SCALES + wr * P::FACTORS + col * 4;
+        const uint8_t *zero = here + P::ZEROS + wo * P::FACTORS / 4 + col;
+        u32x4 w[4], b[2][4];
+        uint32_t z[4];
+        auto read_rows = [&](int phase) {           // (8 bits: one load holds 64 inputs)
+            const int t = X == ROWS_I8 ? phase * WIDE / 2 : phase;
+            if (X == ROWS_I8 && WIDE == 1 && phase % 2) return;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) total[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), b[j], total[i][j], 0, 0, 0);
+            for (int j = 0; j < 4; ++j) b[t & 1][j] = *reinterpret_cast<const u32x4 *>(x + j * TB + t * 1024);
+        };
+        read_rows(0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const u32x4 *>(wc + i * 1024);
+        fetch(min(s + AHEAD, steps - 1), place == 0 ? BUFFERS - 1 : place - 1);          // (past the end: the last chunk once more, which nobody reads)
+        place = place == BUFFERS - 1 ? 0 : place + 1;
+#pragma unroll
+        for (int phase = 0; phase < PHASES; ++phase) {
+            const bool starts = phase * WIDE % STEPS == 0;
+            const int g = phase * WIDE / STEPS, t = X == ROWS_I8 ? phase * WIDE / 2 : phase;
+            if (X == ROWS_I8 && starts)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[i] = zero[(i * PER_CHUNK + g) * 16] * 0x01010101u;
+            if (phase + 1 < PHASES) read_rows(phase + 1);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (starts) {
+                    rescale(i);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[i][j] = typename F::acc_t{0, 0, 0, 0};
+                }
+                if constexpr (X != ROWS_I8) {
+                    const auto wide = F::widen(w[i][phase]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[i][j] = F::mfma(wide, b[t & 1][j], acc[i][j]);
+                } else if constexpr (STEPS == 1) {          // (two groups in the 64 inputs of a load)
+                    const long wide = F::widen(w[i][phase], z[i]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        acc[i][j] = F::mfma(wide, (long)((uint64_t)b[t & 1][j][2 * (phase & 1)] | (uint64_t)b[t & 1][j][2 * (phase & 1) + 1] << 32), acc[i][j]);
+                } else {
+                    const uint32_t c0 = w[i][2 * phase], c1 = w[i][2 * phase + 1];
+                    const i32x4 wide{(int)F::minus(c0, z[i]), (int)F::minus(c0 >> 4, z[i]), (int)F::minus(c1, z[i]), (int)F::minus(c1 >> 4, z[i])};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wide, __builtin_bit_cast(i32x4, b[t & 1][j]), acc[i][j], 0, 0, 0);
+                }
+            }
+            if (starts) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) factor[i] = *reinterpret_cast<const f32x4 *>(sw + (i * PER_CHUNK + g) * 64);
+                if (GROUPED)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) row_factor[j] = *reinterpret_cast<const float *>(sx + (j * PER_CHUNK + g) * 64);
+            }
         }
+        __builtin_amdgcn_s_waitcnt(0xc07f);                           // lgkmcnt(0): its reads of the place are over at the next barrier
+        asm volatile("" ::: "memory");
     }
-    const int pitch = l.tiles * TILE;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) rescale(i);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int row = (rtile + j) * TILE + col;
         if (row >= a.rows) continue;
-        if (a.shares > 1) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (otile + i < l.tiles)
-                    *reinterpret_cast<f32x4 *>(a.partial + ((size_t)share * a.rows + row) * pitch + (otile + i) * TILE + 4 * quarter) = total[i][j];
-            continue;
-        }
         const float c = X == ROWS_I8 && !GROUPED ? a.x_scale[row] : 1.0f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -304,69 +331,199 @@ __global__ __launch_bounds__(256, 2) void w4_tiles_kernel(TileArgs a)
             store_four(a.y, a.type, (size_t)row * a.out + o, v, a.out - o);
         }
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                     // (the loads past the end are into this workgroup's LDS)
 }
 
-// The shares of a result added in their order.
-__global__ __launch_bounds__(256) void w4_join_kernel(const float *partial, const float *row_scale, void *y, int rows, int out, int shares, int type)
+// The same sums where there are too few tiles of that size: a workgroup makes 64 outputs x 64 rows, its eight waves take every eighth chunk (its parts
+// one after another), operands straight to registers, and add their sums in LDS.
+template <int X, int STEPS, bool GROUPED>
+__global__ __launch_bounds__(512) void w4_waves_kernel(TileArgs a)
 {
-    const int pitch = (out + TILE - 1) / TILE * TILE, quads = pitch / 4;
-    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= (size_t)rows * quads) return;
-    const size_t row = i / quads;
-    const int o = (int)(i % quads) * 4;
-    f32x4 v{0, 0, 0, 0};
-    for (int s = 0; s < shares; ++s) v += *reinterpret_cast<const f32x4 *>(partial + ((size_t)s * rows + row) * pitch + o);
-    if (row_scale) v *= row_scale[row];
-    store_four(y, type, row * out + o, v, out - o);
+    typedef Form<X> F;
+    constexpr int WAVES = 8, TB = X == ROWS_I8 ? 2048 : 4096, PER_CHUNK = 4 / STEPS, PITCH = 68;
+    extern __shared__ __attribute__((aligned(16))) float red[];             // [WAVES][64 rows][PITCH]
+    const W4Layout l(a.out, a.in, 32 * STEPS);
+    const Staged st(a.rows, a.in, 32 * STEPS, a.form);
+    const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quarter = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int otile = blockIdx.x * 4, rtile = blockIdx.y * 4;
+    const u32x4 *codes[4];
+    const float *scales[4];
+    const uint8_t *zeros[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const size_t tile = min(otile + i, l.tiles - 1);
+        codes[i] = reinterpret_cast<const u32x4 *>(a.image) + tile * l.chunks * 64 + lane;
+        scales[i] = reinterpret_cast<const float *>(a.image + l.scale_at()) + tile * l.groups * 16;
+        zeros[i] = a.image + l.zero_at() + tile * l.groups * 16 + col;
+    }
+    const float *row_scales = reinterpret_cast<const float *>(a.staged + st.scales_at()) + (size_t)rtile * l.groups * 16 + col;
+    const u32x4 *rows_from = reinterpret_cast<const u32x4 *>(a.staged + ((size_t)(rtile / BLOCK) * st.chunks * st.parts * BLOCK + rtile % BLOCK) * TB) + lane;
+    f32x4 total[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) total[i][j] = f32x4{0, 0, 0, 0};
+    constexpr int READS = TB / 1024;
+    const int steps = st.chunks * st.parts;
+    for (int s = wave; s < steps; s += WAVES) {
+        const int chunk = st.parts == 1 ? s : (int)(__umulhi((uint32_t)s, 0xaaaaaaabu) >> 1);
+        // (all loads of a step at once: their trips are what a step takes)
+        u32x4 w[4], b[READS][4];
+        f32x4 f[PER_CHUNK][4];
+        float c[PER_CHUNK][4];
+        uint32_t z[PER_CHUNK][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = codes[i][(size_t)chunk * 64];
+#pragma unroll
+        for (int t = 0; t < READS; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[t][j] = rows_from[(size_t)s * (BLOCK * TB / 16) + j * (TB / 16) + t * 64];
+#pragma unroll
+        for (int n = 0; n < PER_CHUNK; ++n) {
+            const size_t g = min(chunk * PER_CHUNK + n, l.groups - 1) * 16;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                f[n][i] = *reinterpret_cast<const f32x4 *>(scales[i] + g + 4 * quarter);
+                if (X == ROWS_I8) z[n][i] = zeros[i][g];
+                if (GROUPED) c[n][i] = row_scales[(size_t)i * l.groups * 16 + g];
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            typename F::acc_t acc[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const uint32_t zero = X == ROWS_I8 ? z[t / STEPS][i] * 0x01010101u : 0;
+                if (t % STEPS == 0)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[j] = typename F::acc_t{0, 0, 0, 0};
+                if constexpr (X != ROWS_I8) {
+                    const auto wide = F::widen(w[i][t]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[j] = F::mfma(wide, b[t][j], acc[j]);
+                } else if constexpr (STEPS == 1) {          // (two groups in the 64 inputs of a load)
+                    const long wide = F::widen(w[i][t], zero);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        acc[j] = F::mfma(wide, (long)((uint64_t)b[t / 2][j][2 * (t & 1)] | (uint64_t)b[t / 2][j][2 * (t & 1) + 1] << 32), acc[j]);
+                } else if (t % 2 == 0) {
+                    const i32x4 wide{(int)F::minus(w[i][t], zero), (int)F::minus(w[i][t] >> 4, zero), (int)F::minus(w[i][t + 1], zero),
+                                     (int)F::minus(w[i][t + 1] >> 4, zero)};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wide, __builtin_bit_cast(i32x4, b[t / 2][j]), acc[j], 0, 0, 0);
+                }
+                if (t % STEPS != STEPS - 1) continue;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        float part = (float)acc[j][v];
+                        if (GROUPED) part *= c[t / STEPS][j];
+                        total[i][j][v] = __builtin_fmaf(f[t / STEPS][i][v], part, total[i][j][v]);
+                    }
+            }
+        }
+    }
+    if constexpr (X != ROWS_I8) {                   // the offset and the zero points, as in w4_tiles_kernel
+        const u32x4 *sums = reinterpret_cast<const u32x4 *>(a.staged + st.sums_at()) + (size_t)rtile * st.quads * 64 + lane;
+        for (int quad = wave; quad < st.quads; quad += WAVES) {
+            bf16x8 b[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[j] = __builtin_bit_cast(bf16x8, sums[((size_t)j * st.quads + quad) * 64]);
+            const int g = min(4 * quad + quarter, l.groups - 1);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bf16x8 k = offset_parts<X>(scales[i][(size_t)g * 16 + col], zeros[i][(size_t)g * 16]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) total[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, b[j], total[i][j], 0, 0, 0);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4 *>(red + (wave * 64 + 16 * j + col) * PITCH + 16 * i + 4 * quarter) = total[i][j];
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        const int r = (tid >> 4) + 32 * p, q = (tid & 15) * 4, row = rtile * TILE + r, o = otile * TILE + q;
+        if (row >= a.rows) continue;
+        f32x4 v = *reinterpret_cast<const f32x4 *>(red + r * PITCH + q);
+#pragma unroll
+        for (int k = 1; k < WAVES; ++k) v += *reinterpret_cast<const f32x4 *>(red + (k * 64 + r) * PITCH + q);
+        if (X == ROWS_I8 && !GROUPED) v *= a.x_scale[row];
+        store_four(a.y, a.type, (size_t)row * a.out + o, v, a.out - o);
+    }
 }
 
-struct Shares {
-    int count, chunks;
-};
-// Shares of the inputs: until there are two workgroups per CU.
-Shares shares_of(int rows, int in, int out)
-{
-    const int chunks = (in + 127) / 128, longest = (chunks + SPLIT_CHUNKS - 1) / SPLIT_CHUNKS;
-    const long long tiles = (long long)((rows + 127) / 128) * ((out + 127) / 128);
-    const int want = (int)std::max<long long>(1, std::min<long long>({512 / tiles, longest, 16}));
-    const int per = (longest + want - 1) / want * SPLIT_CHUNKS;
-    return {(chunks + per - 1) / per, per};
-}
+constexpr int SIDE = 4;             // waves of w4_tiles_kernel along the outputs, 64 of them each
 
-template <int X, bool GROUPED> xnor_status launch_tiles(const TileArgs &a, hipStream_t stream)
+template <int X, bool GROUPED> xnor_status launch_waves(const TileArgs &a, int group, hipStream_t stream)
 {
-    const int tb = X == ROWS_I8 ? 2048 : 4096, factors = BLOCK * (128 / a.group) * (64 * (GROUPED ? 2 : 1) + (X == ROWS_I8 ? 16 : 0));
-    const unsigned lds = 2 * (BLOCK * tb + factors);
-    const long long count = (long long)a.row_blocks * a.out_blocks * a.shares;
-    if (count > 0x7fffff00 / 256) return XNOR_ERR_SHAPE;
-    const dim3 grid((unsigned)((count + 7) / 8 * 8));
+    constexpr unsigned lds = 8 * 64 * 68 * sizeof(float);
+    const dim3 grid((unsigned)((a.out + 63) / 64), (unsigned)((a.rows + 63) / 64));
     auto go = [&](auto kernel) {
-        if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
-            return XNOR_ERR_HIP;
-        kernel<<<grid, dim3(256), lds, stream>>>(a);
+        if (hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) return XNOR_ERR_HIP;
+        kernel<<<grid, dim3(512), lds, stream>>>(a);
         return hip_status(hipGetLastError());
     };
-    if (a.group == 32) return go(w4_tiles_kernel<X, 1, GROUPED>);
-    if (a.group == 64) return go(w4_tiles_kernel<X, 2, GROUPED>);
-    return go(w4_tiles_kernel<X, 4, GROUPED>);
+    if (group == 32) return go(w4_waves_kernel<X, 1, GROUPED>);
+    if (group == 64) return go(w4_waves_kernel<X, 2, GROUPED>);
+    return go(w4_waves_kernel<X, 4, GROUPED>);
+}
+
+template <int X, bool GROUPED> xnor_status launch_tiles(const TileArgs &a, int group, hipStream_t stream)
+{
+    constexpr int BUFFERS = X == ROWS_I8 ? 4 : 3;
+    const long long count = (long long)a.row_blocks * a.out_blocks;
+    if (count > 0xffffff00LL / (128 * SIDE)) return XNOR_ERR_SHAPE;
+    const dim3 grid((unsigned)((count + 7) / 8 * 8));
+    auto go = [&](auto kernel, unsigned lds) {
+        if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
+            return XNOR_ERR_HIP;
+        kernel<<<grid, dim3(128 * SIDE), lds, stream>>>(a);
+        return hip_status(hipGetLastError());
+    };
+    if (group == 32) return go(w4_tiles_kernel<X, 1, GROUPED, SIDE, BUFFERS>, BUFFERS * TilePlace<X, 1, GROUPED, SIDE>::BYTES);
+    if (group == 64) return go(w4_tiles_kernel<X, 2, GROUPED, SIDE, BUFFERS>, BUFFERS * TilePlace<X, 2, GROUPED, SIDE>::BYTES);
+    return go(w4_tiles_kernel<X, 4, GROUPED, SIDE, BUFFERS>, BUFFERS * TilePlace<X, 4, GROUPED, SIDE>::BYTES);
 }
 
 }  // namespace
 
-bool w4_tiles_applies(int rows) { return rows > 64; }
-
-size_t w4_tiles_workspace_bytes(int rows, int in, int out, int group)
+// Which kernel takes a product: the shortest of three times in us, fitted to 60 products (inputs 1003 to 9216, outputs 1000 to 16384, 17 to 2048 rows;
+// chunks are of 128 inputs, rounds of 256 workgroups).  Up to 16 rows w4_rows_kernel reads the codes at the memory's rate and nothing can be
+// ahead of it.  With more it makes up to 32 or 64 rows by 16 outputs per workgroup, every one of which reads all rows' inputs again, but is one launch:
+// 17 bfloat16 rows 9216 -> 4096 14 us against 26 by waves and 23 by tiles, 64 rows 36, 26 and 27, 128 rows 2048 -> 2048 11, 14 and 24.  The others
+// stage the rows first.  Tiles of 64 x 64 whose inputs eight waves share fill the chip where few of 256 x 128 would not (512 rows 4096 -> 4096 35 us
+// against 42, 256 rows 4096 -> 16384 55 and 50); 2048 rows 4096 -> 8192: 189 and 148.
+W4Kernel w4_kernel(int rows, int in, int out, int form)
 {
-    const Shares s = shares_of(rows, in, out);
-    const size_t partial = s.count > 1 ? (size_t)s.count * rows * ((out + TILE - 1) / TILE * TILE) * sizeof(float) : 0;
-    return std::max(Staged(rows, in, group, ROWS_F32).partial_at(), Staged(rows, in, group, ROWS_I8).partial_at()) + partial;
+    if (rows <= TILE) return W4_ROWS;
+    const double chunks = (in + 127) / 128, parts = form == ROWS_F32 ? 3 : 1;
+    auto rounds = [&](int outs, int height) { return std::ceil((double)((out + outs - 1) / outs) * ((rows + height - 1) / height) / 256); };
+    const bool two = rows <= 2 * TILE, wide = two && out > 511 * TILE;
+    const double by_rows = 4 + (two ? 0.24 : 0.43) * (parts > 1 ? 1.5 : 1) * chunks * rounds(wide ? 32 : 16, 64);
+    const double waves = rounds(64, 64), by_waves = 9 + (waves > 1 ? 2.8 : 2.0) * std::ceil(chunks * parts / 8) * waves;
+    const double by_tiles = 8 + 2.1 * chunks * parts * rounds(64 * SIDE, TILE * BLOCK);
+    if (by_rows <= by_waves && by_rows <= by_tiles) return W4_ROWS;
+    return by_waves <= by_tiles ? W4_WAVES : W4_TILES;
 }
 
-xnor_status launch_w4_tiles(const void *x, long long x_stride, const float *x_scale, const void *wimg, void *y, void *workspace, int rows, int in, int out,
-                            int group, int x_group, int form, int type, hipStream_t stream)
+size_t w4_staged_bytes(int rows, int in, int out, int group)
+{
+    size_t most = 0;
+    for (int form : {(int)ROWS_F32, (int)ROWS_BF16, (int)ROWS_I8})
+        if (w4_kernel(rows, in, out, form) != W4_ROWS) most = std::max(most, Staged(rows, in, group, form).total());
+    return most;
+}
+
+xnor_status launch_w4_staged(W4Kernel kernel, const void *x, long long x_stride, const float *x_scale, const void *wimg, void *y, void *workspace, int rows,
+                             int in, int out, int group, int x_group, int form, int type, hipStream_t stream)
 {
     const Staged st(rows, in, group, form);
-    const Shares s = shares_of(rows, in, out);
     uint8_t *staged = static_cast<uint8_t *>(workspace);
     const StageArgs sa{x, x_scale, staged, x_stride, rows, in, group, x_group, x_group ? (in + x_group - 1) / x_group : 1};
     const dim3 grid((unsigned)((st.chunks + 3) / 4), (unsigned)((rows + TILE - 1) / TILE));
@@ -375,17 +532,15 @@ xnor_status launch_w4_tiles(const void *x, long long x_stride, const float *x_sc
     else if (form == ROWS_F16) w4_stage_kernel<ROWS_F16><<<grid, dim3(256), 0, stream>>>(sa);
     else w4_stage_kernel<ROWS_I8><<<grid, dim3(256), 0, stream>>>(sa);
     if (xnor_status e = hip_status(hipGetLastError())) return e;
-    const TileArgs a{staged, static_cast<const uint8_t *>(wimg), x_scale, reinterpret_cast<float *>(staged + st.partial_at()), y, rows, in, out, group,
-                     type, form, st.blocks, (out + TILE * BLOCK - 1) / (TILE * BLOCK), s.count, s.chunks};
-    xnor_status e;
-    if (form == ROWS_I8) e = x_group ? launch_tiles<ROWS_I8, true>(a, stream) : launch_tiles<ROWS_I8, false>(a, stream);
-    else if (form == ROWS_F16) e = launch_tiles<ROWS_F16, false>(a, stream);
-    else e = launch_tiles<ROWS_BF16, false>(a, stream);
-    if (e != XNOR_OK || s.count == 1) return e;
-    const size_t quads = (size_t)rows * ((out + TILE - 1) / TILE * 4);
-    w4_join_kernel<<<dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, stream>>>(a.partial, form == ROWS_I8 && !x_group ? x_scale : nullptr, y, rows, out,
-                                                                                    s.count, type);
-    return hip_status(hipGetLastError());
+    const TileArgs a{staged, static_cast<const uint8_t *>(wimg), x_scale, y, rows, in, out, type, form, st.blocks, (out + 64 * SIDE - 1) / (64 * SIDE)};
+    if (kernel == W4_WAVES) {
+        if (form == ROWS_I8) return x_group ? launch_waves<ROWS_I8, true>(a, group, stream) : launch_waves<ROWS_I8, false>(a, group, stream);
+        if (form == ROWS_F16) return launch_waves<ROWS_F16, false>(a, group, stream);
+        return launch_waves<ROWS_BF16, false>(a, group, stream);
+    }
+    if (form == ROWS_I8) return x_group ? launch_tiles<ROWS_I8, true>(a, group, stream) : launch_tiles<ROWS_I8, false>(a, group, stream);
+    if (form == ROWS_F16) return launch_tiles<ROWS_F16, false>(a, group, stream);
+    return launch_tiles<ROWS_BF16, false>(a, group, stream);
 }
 
 }  // namespace xnor

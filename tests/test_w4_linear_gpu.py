@@ -70,6 +70,33 @@ def test_products_of_many_rows(t, rows, out, cin, group):
     check(packed, w, top, normal(gen, rows, cin).to(TYPES[t]), t, group)
 
 
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16", "q8"])
+@pytest.mark.parametrize("rows,out,cin,group", [(2100, 8200, 520, 32), (2049, 8192, 384, 64), (2050, 8190, 640, 128)])
+def test_products_of_very_many_rows(t, rows, out, cin, group):
+    """Enough results for the largest tiles; the first and last rows and some between are looked at."""
+    gen = generator(rows)
+    packed, w, top = make(gen, out, cin, group, True)
+    some = torch.cat((torch.arange(130), torch.randint(0, rows, (64,), generator=gen), torch.arange(rows - 66, rows)))
+    if t != "q8":
+        x = normal(gen, rows, cin).to(TYPES[t])
+        y = product(packed, x, t, rows, cin, out, group)[some.cuda()]
+        want = x[some].double() @ w.t()
+        rms = x[some].double().square().mean(1).sqrt()
+        assert_within(y, want, 4 * cin * 62 * EPS32 * rms[:, None] * top[None] + HALF_ULP[t] * want.abs() + SMALLEST[t], "y")
+        return
+    for x_group in (0, 128):
+        q = torch.randint(-127, 128, (rows, cin), generator=gen, dtype=torch.int8)
+        xs = torch.rand((rows, -(-cin // x_group) if x_group else 1), generator=gen) + 0.5
+        y = filled((rows, out), torch.float32)
+        xnor.xnor_w4_linear_q8(q.cuda(), xs.cuda(), packed.wimg, y, scratch(rows, cin, out, group), rows, cin, out, group, x_group)
+        want = sums = 0
+        for k in range(0, cin, group):
+            whole = torch.round(w[:, k:k + group] / packed.test_scale[:, k // group, None])
+            part = (q[some, k:k + group].double() @ whole.t()) * packed.test_scale[:, k // group] * xs[some].double()[:, k // x_group if x_group else 0, None]
+            want, sums = want + part, sums + part.abs()
+        assert_within(y[some.cuda()], want, (-(-cin // group) + 8) * 2 * EPS32 * sums + HALF_ULP["f32"] * want.abs(), "y")
+
+
 @pytest.mark.parametrize("t,extra", [("f32", 1), ("bf16", 3), ("f16", 8), ("bf16", 8)])
 @pytest.mark.parametrize("rows", [3, 40, 200])
 def test_rows_that_lie_apart(t, extra, rows):
