@@ -5,7 +5,7 @@
 
 namespace xnor {
 
-int rmsnorm_grad_parts(int rows);           // shares of g_weight, [parts][cols] floats
+int rmsnorm_grad_parts(int rows, int cols);         // shares of g_weight, [parts][cols] floats
 xnor_status launch_rmsnorm_q8(const void *x, long long x_stride, const void *residual, long long residual_stride, const float *weight,
                               void *sum_out, int8_t *q, float *scale, void *values, float *rstd, int rows, int cols, int group, int type,
                               float eps, hipStream_t stream);

@@ -45,7 +45,7 @@ int xnor_rmsnorm_q8(const void *x, int64_t x_stride, const void *residual, int64
 size_t xnor_rmsnorm_backward_workspace_bytes(int rows, int cols)
 {
     if (rows <= 0 || rows > MAX_ROWS || cols <= 0 || cols > MAX_COLS) return 0;
-    return (size_t)rmsnorm_grad_parts(rows) * (size_t)cols * sizeof(float);
+    return (size_t)rmsnorm_grad_parts(rows, cols) * (size_t)cols * sizeof(float);
 }
 
 int xnor_rmsnorm_backward(const void *h, int64_t h_stride, const float *rstd, const float *weight, const void *g_values, int64_t g_stride,

@@ -2,6 +2,7 @@
 #include "xnor_internal.h"
 #include "real8.h"
 #include "lowbit.h"
+#include <algorithm>
 
 namespace xnor {
 
@@ -9,8 +10,8 @@ namespace {
 
 constexpr float TINY = 0x1p-100f;           // groups whose largest magnitude is below hold zeros
 
-// Sum over the workgroup, the same value in every thread; `slots` holds a float per wave.
-__device__ __forceinline__ float workgroup_sum(float v, float *slots)
+// Sum over the threads of a row (blockDim.x, whole waves), the same value in all of them; `slots` holds a float per wave of the row.
+__device__ __forceinline__ float row_sum(float v, float *slots)
 {
     v = wave_sum(v);
     const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
@@ -152,21 +153,24 @@ struct NormGradArgs {
     int rows, cols;
 };
 
-// A workgroup takes every gridDim.x-th row, its threads the same columns of each (as the forward kernel), whose shares of g_weight stay in
-// registers until the end.
+// blockDim.y rows at a time, each by blockDim.x threads (as in the forward kernel), and every gridDim.x-th such set per workgroup: a thread meets the
+// same columns of each, whose shares of g_weight stay in its registers until the end, when those of the rows side by side are added in LDS.
 template <int TYPE, int STEPS>
 __global__ __launch_bounds__(1024) void rmsnorm_grad_kernel(NormGradArgs a)
 {
     typedef real_t<TYPE> T;
     __shared__ float sums[2][16];
-    const int tid = threadIdx.x;
+    extern __shared__ __attribute__((aligned(16))) float side[];               // [blockDim.y - 1][cols]
+    const int tid = threadIdx.x, beside = __builtin_amdgcn_readfirstlane(threadIdx.y);      // (a row's threads are whole waves)
     float gw[STEPS][8];
 #pragma unroll
     for (int i = 0; i < STEPS; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j) gw[i][j] = 0.0f;
     int turn = 0;
-    for (int row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+    for (int first = blockIdx.x * (int)blockDim.y; first < a.rows; first += gridDim.x * blockDim.y, turn ^= 1) {
+        const bool real = first + beside < a.rows;      // (threads past the last row take it once more, and leave nothing)
+        const int row = real ? first + beside : a.rows - 1;
         const T *h = static_cast<const T *>(a.h) + (size_t)row * a.h_stride;
         const T *g = static_cast<const T *>(a.g) + (size_t)row * a.g_stride;
         const T *gs = static_cast<const T *>(a.g_sum) + (a.g_sum ? (size_t)row * a.g_sum_stride : 0);
@@ -195,11 +199,12 @@ __global__ __launch_bounds__(1024) void rmsnorm_grad_kernel(NormGradArgs a)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float n = hv[i][j] * rstd, p = gv[i][j] * n;
-                gw[i][j] += p;
+                if (real) gw[i][j] += p;
                 dot += a.weight ? p * w[j] : p;
             }
         }
-        dot = workgroup_sum(dot, sums[turn]) / (float)a.cols;
+        dot = row_sum(dot, sums[turn] + beside * (blockDim.x >> 6)) / (float)a.cols;
+        if (!real) continue;
         T *out = static_cast<T *>(a.g_h) + (size_t)row * a.cols;
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
@@ -221,6 +226,26 @@ __global__ __launch_bounds__(1024) void rmsnorm_grad_kernel(NormGradArgs a)
         }
     }
     if (!a.partial) return;
+    if (blockDim.y > 1) {
+        if (beside)
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int c = 8 * (tid + i * (int)blockDim.x) + j;
+                    if (c < a.cols) side[(beside - 1) * a.cols + c] = gw[i][j];
+                }
+        __syncthreads();
+        if (beside) return;
+        for (int k = 0; k < (int)blockDim.y - 1; ++k)
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int c = 8 * (tid + i * (int)blockDim.x) + j;
+                    if (c < a.cols) gw[i][j] += side[k * a.cols + c];
+                }
+    }
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
         const int c = 8 * (tid + i * (int)blockDim.x);
@@ -239,7 +264,7 @@ __global__ __launch_bounds__(1024) void rmsnorm_grad_sum_kernel(const float *__r
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
     float s = 0.0f;
     if (c < cols)
-#pragma unroll 8
+#pragma unroll 16
         for (int p = wave; p < parts; p += 16) s += partial[(size_t)p * cols + c];
     sums[wave][lane] = s;
     __syncthreads();
@@ -249,7 +274,7 @@ __global__ __launch_bounds__(1024) void rmsnorm_grad_sum_kernel(const float *__r
     g_weight[c] = s;
 }
 
-// Steps of eight columns per thread and threads per workgroup for rows of `cols`.
+// Steps of eight columns per thread and threads per row.
 struct RowShape {
     int steps, threads;
 };
@@ -268,7 +293,21 @@ template <class F> void by_steps(int steps, F f)
 
 }  // namespace
 
-int rmsnorm_grad_parts(int rows) { return rows < 512 ? rows : 512; }
+// How the backward pass shares out its rows: eight waves of rows side by side (a row's trip to memory and back would be all that a narrow row's
+// workgroup waits for), and as many workgroups as take the same number of turns each, or one less: two per CU, one of the widest rows, whose shares of
+// g_weight weigh more than what a second workgroup hides.  8000 x 100 float32 one row at a time 31 us, eight 12; 2048 x 9216 bfloat16 two per CU 45, one 42;
+// 2048 x 4096 18 and 20.
+struct GradShape {
+    int beside, parts;
+};
+static GradShape grad_shape(int rows, int cols)
+{
+    if (rows == 0) return {1, 0};
+    const int waves = row_shape(cols).threads / 64, beside = std::max(1, 8 / waves), most = waves > 8 ? 256 : 512;
+    const int sets = (rows + beside - 1) / beside, turns = (sets + most - 1) / most;
+    return {beside, (sets + turns - 1) / turns};
+}
+int rmsnorm_grad_parts(int rows, int cols) { return grad_shape(rows, cols).parts; }
 
 xnor_status launch_rmsnorm_q8(const void *x, long long x_stride, const void *residual, long long residual_stride, const float *weight,
                               void *sum_out, int8_t *q, float *scale, void *values, float *rstd, int rows, int cols, int group, int type,
@@ -287,13 +326,17 @@ xnor_status launch_rmsnorm_backward(const void *h, long long h_stride, const flo
                                     const void *g_sum, long long g_sum_stride, void *g_h, float *g_weight, void *workspace, int rows, int cols,
                                     int type, hipStream_t stream)
 {
-    const int parts = rmsnorm_grad_parts(rows);
+    const GradShape shape = grad_shape(rows, cols);
+    const int parts = shape.parts;
     if (rows > 0) {
         const NormGradArgs a{h, g, g_sum, rstd, weight, g_h, g_weight ? static_cast<float *>(workspace) : nullptr, h_stride, g_stride,
                              g_sum_stride, rows, cols};
         const RowShape s = row_shape(cols);
         by_type(type, [&](auto t) {
-            by_steps(s.steps, [&](auto n) { rmsnorm_grad_kernel<t(), n()><<<dim3((unsigned)parts), dim3((unsigned)s.threads), 0, stream>>>(a); });
+            by_steps(s.steps, [&](auto n) {
+                rmsnorm_grad_kernel<t(), n()><<<dim3((unsigned)parts), dim3((unsigned)s.threads, (unsigned)shape.beside),
+                                                (size_t)(shape.beside - 1) * cols * sizeof(float), stream>>>(a);
+            });
         });
         if (xnor_status e = hip_status(hipGetLastError())) return e;
     }
