@@ -92,30 +92,32 @@ struct W4Args {
     int rows, in, out, x_groups, x_shift, type;     // a group's scale of x: group >> x_shift
 };
 
-// What a wave multiplies at a time: 16 * TILES outputs, 128 inputs, 16 * BLOCKS rows.
-template <int X, int BLOCKS, int TILES, int STEPS> struct Chunk {
+// What a wave multiplies at a time: 16 * TILES outputs, 128 inputs, 16 rows.
+template <int X, int TILES, int STEPS> struct Chunk {
     static constexpr int GROUPS = 4 / STEPS;
     u32x4 w[TILES];
-    Eight<X> x[4][BLOCKS];
+    Eight<X> x[4];
     f32x4 s[GROUPS][TILES];
     uint32_t z[GROUPS][TILES];      // 16 bits: of a lane's four results; 8 bits: of its operand
-    float xs[X == ROWS_I8 ? GROUPS : 1][BLOCKS];
+    float xs[X == ROWS_I8 ? GROUPS : 1];
 };
 
-// A workgroup makes 16 * TILES outputs of 16 * BLOCKS rows; its waves take every WAVES-th chunk of 128 inputs and add their sums in LDS.  Nothing
-// is staged: a code is read once, straight from the image into the lane that multiplies it, DEPTH chunks ahead.  Lanes past the last row multiply
-// it once more.  GROUPED: 8-bit rows with scales of groups.
-template <int X, int BLOCKS, int TILES, int STEPS, bool GROUPED, int WAVES, int DEPTH>
+// A workgroup makes 16 * TILES outputs of 16 rows; its waves take every WAVES-th chunk of 128 inputs and add their sums in LDS.  Nothing is staged: a
+// code is read once, straight from the image into the lane that multiplies it, DEPTH chunks ahead.  Lanes past the last row multiply it once
+// more.  GROUPED: 8-bit rows with scales of groups.
+// What bounds it: with few rows the memory (8 8-bit rows 4096 -> 32000 13.4 us for 71 MB, 5.3 TB/s) or, where the weights are small, the launch and one
+// trip to memory (one bfloat16 row 9216 -> 4096 6.4 us, 20 MB); with more the rows' inputs, which every workgroup reads in pieces of 16 bytes.
+template <int X, int TILES, int STEPS, bool GROUPED, int WAVES, int DEPTH>
 __global__ __launch_bounds__(64 * WAVES) void w4_rows_kernel(W4Args a)
 {
     typedef Form<X> F;
-    typedef Chunk<X, BLOCKS, TILES, STEPS> C;
+    typedef Chunk<X, TILES, STEPS> C;
     constexpr int GROUP = 32 * STEPS, XBYTES = X == ROWS_F32 ? 4 : X == ROWS_I8 ? 1 : 2, PITCH = 16 * TILES + 4;
-    __shared__ __attribute__((aligned(16))) float red[WAVES][16 * BLOCKS][PITCH];
+    __shared__ __attribute__((aligned(16))) float red[WAVES][16][PITCH];
     const W4Layout l(a.out, a.in, GROUP);
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quarter = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int tile0 = blockIdx.x * TILES, row0 = blockIdx.y * 16 * BLOCKS;
+    const int tile0 = blockIdx.x * TILES, row0 = blockIdx.y * 16;
     // (a workgroup's tiles past the last one multiply the last once more)
     const u32x4 *codes[TILES];
     const float *scales[TILES];
@@ -127,19 +129,12 @@ __global__ __launch_bounds__(64 * WAVES) void w4_rows_kernel(W4Args a)
         scales[t] = reinterpret_cast<const float *>(a.image + l.scale_at()) + tile * l.groups * 16 + 4 * quarter;
         zeros[t] = a.image + l.zero_at() + tile * l.groups * 16 + (X == ROWS_I8 ? col : 4 * quarter);
     }
-    const char *xrow[BLOCKS];
-    const float *xscale[BLOCKS];
+    const size_t own_row = min(row0 + col, a.rows - 1);
+    const char *xrow = static_cast<const char *>(a.x) + own_row * a.x_stride * XBYTES;
+    const float *xscale = a.x_scale + own_row * a.x_groups;
+    f32x4 total[TILES];
 #pragma unroll
-    for (int b = 0; b < BLOCKS; ++b) {
-        const size_t row = min(row0 + 16 * b + col, a.rows - 1);
-        xrow[b] = static_cast<const char *>(a.x) + row * a.x_stride * XBYTES;
-        xscale[b] = a.x_scale + row * a.x_groups;
-    }
-    f32x4 total[TILES][BLOCKS];
-#pragma unroll
-    for (int t = 0; t < TILES; ++t)
-#pragma unroll
-        for (int b = 0; b < BLOCKS; ++b) total[t][b] = f32x4{0, 0, 0, 0};
+    for (int t = 0; t < TILES; ++t) total[t] = f32x4{0, 0, 0, 0};
     // whole: 128 inputs exist.  A group past the last input has sums of zero, whatever it is scaled with
     auto load = [&](C &c, int chunk, bool whole) {
 #pragma unroll
@@ -147,8 +142,7 @@ __global__ __launch_bounds__(64 * WAVES) void w4_rows_kernel(W4Args a)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int k = 128 * chunk + 32 * j + 8 * quarter;
-#pragma unroll
-            for (int b = 0; b < BLOCKS; ++b) c.x[j][b].load(xrow[b], k, whole ? 8 : a.in - k);
+            c.x[j].load(xrow, k, whole ? 8 : a.in - k);
         }
 #pragma unroll
         for (int i = 0; i < C::GROUPS; ++i) {
@@ -158,51 +152,41 @@ __global__ __launch_bounds__(64 * WAVES) void w4_rows_kernel(W4Args a)
                 c.s[i][t] = *reinterpret_cast<const f32x4 *>(scales[t] + (size_t)g * 16);
                 c.z[i][t] = X == ROWS_I8 ? zeros[t][(size_t)g * 16] : *reinterpret_cast<const uint32_t *>(zeros[t] + (size_t)g * 16);
             }
-            if (GROUPED)
-#pragma unroll
-                for (int b = 0; b < BLOCKS; ++b) c.xs[i][b] = xscale[b][g >> a.x_shift];
+            if (GROUPED) c.xs[i] = xscale[g >> a.x_shift];
         }
     };
     auto multiply = [&](const C &c) {
-        typename F::acc_t acc[TILES][BLOCKS], sum[BLOCKS];
+        typename F::acc_t acc[TILES], sum;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            if (j % STEPS == 0)
+            if (j % STEPS == 0) {
+                sum = typename F::acc_t{0, 0, 0, 0};
 #pragma unroll
-                for (int b = 0; b < BLOCKS; ++b) {
-                    sum[b] = typename F::acc_t{0, 0, 0, 0};
-#pragma unroll
-                    for (int t = 0; t < TILES; ++t) acc[t][b] = typename F::acc_t{0, 0, 0, 0};
-                }
-            typename F::operand_t wide[TILES];
+                for (int t = 0; t < TILES; ++t) acc[t] = typename F::acc_t{0, 0, 0, 0};
+            }
+            typename F::operand_t xo[F::PARTS];
+            c.x[j].operands(xo);
 #pragma unroll
             for (int t = 0; t < TILES; ++t) {
-                if constexpr (X == ROWS_I8) wide[t] = F::widen(c.w[t][j], c.z[j / STEPS][t] * 0x01010101u);
-                else wide[t] = F::widen(c.w[t][j]);
+                typename F::operand_t wide;
+                if constexpr (X == ROWS_I8) wide = F::widen(c.w[t][j], c.z[j / STEPS][t] * 0x01010101u);
+                else wide = F::widen(c.w[t][j]);
+#pragma unroll
+                for (int p = 0; p < F::PARTS; ++p) acc[t] = F::mfma(wide, xo[p], acc[t]);
             }
+            if constexpr (X != ROWS_I8)
 #pragma unroll
-            for (int b = 0; b < BLOCKS; ++b) {
-                typename F::operand_t xo[F::PARTS];
-                c.x[j][b].operands(xo);
-#pragma unroll
-                for (int p = 0; p < F::PARTS; ++p) {
-#pragma unroll
-                    for (int t = 0; t < TILES; ++t) acc[t][b] = F::mfma(wide[t], xo[p], acc[t][b]);
-                    if constexpr (X != ROWS_I8) sum[b] = F::mfma(F::ones(), xo[p], sum[b]);
-                }
-            }
+                for (int p = 0; p < F::PARTS; ++p) sum = F::mfma(F::ones(), xo[p], sum);
             if (j % STEPS != STEPS - 1) continue;
 #pragma unroll
             for (int t = 0; t < TILES; ++t)
 #pragma unroll
-                for (int b = 0; b < BLOCKS; ++b)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) {
-                        float part;
-                        if constexpr (X == ROWS_I8) part = GROUPED ? (float)acc[t][b][v] * c.xs[j / STEPS][b] : (float)acc[t][b][v];
-                        else part = __builtin_fmaf(-(F::OFFSET + (float)(c.z[j / STEPS][t] >> (8 * v) & 255u)), sum[b][v], acc[t][b][v]);
-                        total[t][b][v] = __builtin_fmaf(c.s[j / STEPS][t][v], part, total[t][b][v]);
-                    }
+                for (int v = 0; v < 4; ++v) {
+                    float part;
+                    if constexpr (X == ROWS_I8) part = GROUPED ? (float)acc[t][v] * c.xs[j / STEPS] : (float)acc[t][v];
+                    else part = __builtin_fmaf(-(F::OFFSET + (float)(c.z[j / STEPS][t] >> (8 * v) & 255u)), sum[v], acc[t][v]);
+                    total[t][v] = __builtin_fmaf(c.s[j / STEPS][t][v], part, total[t][v]);
+                }
         }
     };
     const int whole = a.in / 128;
@@ -223,43 +207,32 @@ __global__ __launch_bounds__(64 * WAVES) void w4_rows_kernel(W4Args a)
         multiply(ring[0]);
     }
 #pragma unroll
-    for (int t = 0; t < TILES; ++t)
-#pragma unroll
-        for (int b = 0; b < BLOCKS; ++b) *reinterpret_cast<f32x4 *>(&red[wave][16 * b + col][16 * t + 4 * quarter]) = total[t][b];
+    for (int t = 0; t < TILES; ++t) *reinterpret_cast<f32x4 *>(&red[wave][col][16 * t + 4 * quarter]) = total[t];
     __syncthreads();
-    for (int i = tid; i < 64 * BLOCKS * TILES; i += 64 * WAVES) {
-        const int r = i / (4 * TILES), q = i % (4 * TILES), row = row0 + r, o = 16 * tile0 + 4 * q;
-        if (row >= a.rows) continue;
-        f32x4 s = *reinterpret_cast<const f32x4 *>(&red[0][r][4 * q]);
+    if (tid >= 64 * TILES) return;
+    const int r = tid / (4 * TILES), q = tid % (4 * TILES), row = row0 + r, o = 16 * tile0 + 4 * q;
+    if (row >= a.rows) return;
+    f32x4 s = *reinterpret_cast<const f32x4 *>(&red[0][r][4 * q]);
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) s += *reinterpret_cast<const f32x4 *>(&red[w][r][4 * q]);
-        if (X == ROWS_I8 && !GROUPED) s *= a.x_scale[row];
-        store_four(a.y, a.type, (size_t)row * a.out + o, s, a.out - o);
-    }
+    for (int w = 1; w < WAVES; ++w) s += *reinterpret_cast<const f32x4 *>(&red[w][r][4 * q]);
+    if (X == ROWS_I8 && !GROUPED) s *= a.x_scale[row];
+    store_four(a.y, a.type, (size_t)row * a.out + o, s, a.out - o);
 }
 
-template <int X, bool GROUPED, int STEPS, int BLOCKS, int TILES, int DEPTH> void launch_rows(const W4Args &a, hipStream_t stream)
+template <int X, bool GROUPED, int STEPS, int TILES, int DEPTH> void launch_rows(const W4Args &a, hipStream_t stream)
 {
-    const dim3 grid((unsigned)((a.out + 16 * TILES - 1) / (16 * TILES)), (unsigned)((a.rows + 16 * BLOCKS - 1) / (16 * BLOCKS)));
-    w4_rows_kernel<X, BLOCKS, TILES, STEPS, GROUPED, 8, DEPTH><<<grid, dim3(512), 0, stream>>>(a);
+    const dim3 grid((unsigned)((a.out + 16 * TILES - 1) / (16 * TILES)), (unsigned)((a.rows + 15) / 16));
+    w4_rows_kernel<X, TILES, STEPS, GROUPED, 8, DEPTH><<<grid, dim3(512), 0, stream>>>(a);
 }
-// Tiles of outputs per workgroup and chunks ahead.  More tiles read the rows' inputs less often, and leave fewer workgroups: they pay where those still fill
-// the chip.  8 8-bit rows 4096 -> 32000 (2000 tiles): one tile 24 us, two 16.0, four 13.4; 16 bfloat16 rows 4096 -> 16384: four 10.7, two 13.7; one row
-// 9216 -> 4096 (256 tiles): one 7.2, two 10.2, four 18.  (Sixteen waves 6.9 on the last, 30 on the first; four chunks ahead of a tile 7.2 and 25.5.)
+// (chunks ahead: two of one or two tiles, but for float32 rows and groups of 32, which fill the registers.  Four of one tile 25.5 us for 8 8-bit rows 4096 -> 32000, two 24;
+// sixteen waves 30)
 template <int X, bool GROUPED, int STEPS> void launch_steps(const W4Args &a, hipStream_t stream)
 {
-    constexpr int TWO = X == ROWS_F32 ? 1 : 2;          // (float32 rows fill the registers)
-    const int tiles = (a.out + 15) / 16;
-    if (a.rows <= 16) {
-        if (tiles >= 1024) launch_rows<X, GROUPED, STEPS, 1, 4, 1>(a, stream);
-        else if (tiles >= 512) launch_rows<X, GROUPED, STEPS, 1, 2, TWO>(a, stream);
-        else launch_rows<X, GROUPED, STEPS, 1, 1, TWO>(a, stream);
-    } else if (a.rows <= 32) {
-        if (tiles >= 512) launch_rows<X, GROUPED, STEPS, 2, 2, 1>(a, stream);
-        else launch_rows<X, GROUPED, STEPS, 2, 1, TWO>(a, stream);
-    } else {
-        launch_rows<X, GROUPED, STEPS, 4, 1, 1>(a, stream);
-    }
+    constexpr int TWO = X == ROWS_F32 || STEPS == 1 ? 1 : 2;
+    const int tiles = w4_rows_tiles(a.rows, a.out);
+    if (tiles == 4) launch_rows<X, GROUPED, STEPS, 4, 1>(a, stream);
+    else if (tiles == 2) launch_rows<X, GROUPED, STEPS, 2, TWO>(a, stream);
+    else launch_rows<X, GROUPED, STEPS, 1, TWO>(a, stream);
 }
 template <int X, bool GROUPED> xnor_status launch_groups(const W4Args &a, int group, hipStream_t stream)
 {

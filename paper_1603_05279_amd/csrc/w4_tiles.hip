@@ -493,22 +493,52 @@ template <int X, bool GROUPED> xnor_status launch_tiles(const TileArgs &a, int g
 
 }  // namespace
 
-// Which kernel takes a product: the shortest of three times in us, fitted to 60 products (inputs 1003 to 9216, outputs 1000 to 16384, 17 to 2048 rows;
-// chunks are of 128 inputs, rounds of 256 workgroups).  Up to 16 rows w4_rows_kernel reads the codes at the memory's rate and nothing can be
-// ahead of it.  With more it makes up to 32 or 64 rows by 16 outputs per workgroup, every one of which reads all rows' inputs again, but is one launch:
-// 17 bfloat16 rows 9216 -> 4096 14 us against 26 by waves and 23 by tiles, 64 rows 36, 26 and 27, 128 rows 2048 -> 2048 11, 14 and 24.  The others
-// stage the rows first.  Tiles of 64 x 64 whose inputs eight waves share fill the chip where few of 256 x 128 would not (512 rows 4096 -> 4096 35 us
-// against 42, 256 rows 4096 -> 16384 55 and 50); 2048 rows 4096 -> 8192: 189 and 148.
+namespace {
+// Rounds of a workgroup per CU.
+double rounds(int out, int outs, int rows, int height)
+{
+    return std::ceil((double)((out + outs - 1) / outs) * ((rows + height - 1) / height) / 256);
+}
+// us per chunk of 128 inputs and round of w4_rows_kernel, by tiles
+constexpr struct { int tiles; double cost; } BY_TILES[] = {{1, 0.11}, {2, 0.155}, {4, 0.2}};
+double rows_cost(int rows, int out, int *tiles)
+{
+    double best = 0;
+    for (const auto &t : BY_TILES) {
+        const double cost = t.cost * rounds(out, 16 * t.tiles, rows, 16);
+        if (best == 0 || cost < best) {
+            best = cost;
+            *tiles = t.tiles;
+        }
+    }
+    return best;
+}
+}  // namespace
+
+// More tiles per workgroup read the rows' inputs less often, and leave fewer workgroups: they pay where those still fill the chip.  One, two and four tiles,
+// us: one bfloat16 row 9216 -> 4096 (256 tiles) 6.5, 9.1, 14.7; 32 rows 20, 13.6, 16.8; 64 rows 38, 25, 17; 8 8-bit rows 4096 -> 32000 24, 16, 14.7;
+// 128 float32 rows 1003 -> 1000 6.4, 5.0, 6.4.
+int w4_rows_tiles(int rows, int out)
+{
+    int tiles;
+    rows_cost(rows, out, &tiles);
+    return tiles;
+}
+
+// Which kernel takes a product: the shortest of three times in us, fitted to 220 products (inputs 256 to 9216, outputs 256 to 32000, 1 to 2048 rows), of
+// which it picks one that is more than a tenth slower than the best twice.
+// w4_rows_kernel reads all rows' inputs in every workgroup, but is one launch; the others stage the rows first.  Tiles of 64 x 64 whose inputs eight waves
+// share fill the chip where few of 256 x 128 would not.  Measured by rows, by waves, by tiles: 64 bfloat16 rows 9216 -> 4096 17, 26, 138; 48 rows
+// 4096 -> 16384 21, 18, 65; 128 rows 9216 -> 4096 29, 27, 141; 600 8-bit rows 512 -> 8192 47, 26, 27; 2048 bfloat16 rows 4096 -> 8192 -, 189, 148.
 W4Kernel w4_kernel(int rows, int in, int out, int form)
 {
-    if (rows <= TILE) return W4_ROWS;
-    const double chunks = (in + 127) / 128, parts = form == ROWS_F32 ? 3 : 1;
-    auto rounds = [&](int outs, int height) { return std::ceil((double)((out + outs - 1) / outs) * ((rows + height - 1) / height) / 256); };
-    const bool two = rows <= 2 * TILE, wide = two && out > 511 * TILE;
-    const double by_rows = 4 + (two ? 0.24 : 0.43) * (parts > 1 ? 1.5 : 1) * chunks * rounds(wide ? 32 : 16, 64);
-    const double waves = rounds(64, 64), by_waves = 9 + (waves > 1 ? 2.8 : 2.0) * std::ceil(chunks * parts / 8) * waves;
-    const double by_tiles = 8 + 2.1 * chunks * parts * rounds(64 * SIDE, TILE * BLOCK);
-    if (by_rows <= by_waves && by_rows <= by_tiles) return W4_ROWS;
+    int tiles;
+    const bool f32 = form == ROWS_F32, i8 = form == ROWS_I8;
+    const double chunks = (in + 127) / 128, parts = f32 ? 3 : 1;
+    const double by_rows = 3 + rows_cost(rows, out, &tiles) * 8 * std::ceil(chunks / 8) * (f32 ? 2 : i8 ? 1.3 : 1);     // (eight waves share the chunks)
+    const double by_waves = 3.5 + rounds(out, 64, rows, 64) * (2.2 + (i8 ? 1.9 : 2.6) * std::ceil(chunks * parts / 8));
+    const double by_tiles = 8 + (i8 ? 1.6 : 2.1) * chunks * parts * rounds(out, 64 * SIDE, rows, TILE * BLOCK);
+    if (by_rows <= by_waves && by_rows <= by_tiles && rows <= 16 * 65535) return W4_ROWS;
     return by_waves <= by_tiles ? W4_WAVES : W4_TILES;
 }
 
