@@ -9,7 +9,7 @@ namespace xnor {
 namespace {
 
 constexpr int THREADS = 256, STEPS = 4, CHUNK = THREADS * 8 * STEPS;      // logits that a workgroup holds in registers at a time
-constexpr int KEPT = 256;                                                 // candidates that wait for each other before the best are chosen
+constexpr int MOST_PARTS = 64, MOST_TOP = 32;
 constexpr int GROUP_LANES = 4, GROUPS = THREADS / GROUP_LANES;            // threads whose largest logits are compared as one
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.693147180559945309417f;
 
@@ -64,11 +64,11 @@ __device__ __forceinline__ void wave_fence()
 }
 
 struct TopLds {
-    key_t list[32];             // the best so far, in order; filled up with none_key()
+    key_t list[MOST_TOP];            // the best so far, in order; filled up with none_key()
     key_t group[GROUPS];
     uint32_t short_group[GROUPS];
     int count;                  // of found
-    key_t found[];              // up to KEPT + top * GROUP_LANES * (keys per thread)
+    key_t found[];              // up to top * parts
 };
 
 // The next float above v (finite; +0 above -0).
@@ -128,7 +128,7 @@ __device__ __forceinline__ void select_top(TopLds &t, int n, int top)
 {
     // a long list is thinned out first: 32 of 64 groups can hold what is not below the threshold, so its length falls to half or less
     while (n > THREADS) {
-        constexpr int MOST = (KEPT + 32 * GROUP_LANES * 32 + THREADS - 1) / THREADS;
+        constexpr int MOST = MOST_PARTS * MOST_TOP / THREADS;
         key_t best = 0;
         for (int i = threadIdx.x; i < n; i += THREADS) best = max(best, t.found[i]);
         __syncthreads();                                        // (t.group is read no more)
@@ -191,13 +191,14 @@ template <int TYPE> __device__ __forceinline__ Given given_at(const LogprobArgs 
     return {real, real ? (float)(static_cast<const real_t<TYPE> *>(a.logits) + row * (size_t)a.stride)[token] : 0.0f};
 }
 
-// A row's results from its statistics and the list of alternatives (all threads of the workgroup).
-template <int TYPE>
+// A row's results from its statistics and the list of alternatives, by the workgroup or, WIDTH = 64, a wave of it.
+template <int TYPE, int WIDTH = THREADS>
 __device__ __forceinline__ void finish_row(const LogprobArgs &a, size_t row, Stats st, const key_t *list, Given own)
 {
+    const int i = threadIdx.x % WIDTH;
     const bool empty = st.m == -__builtin_inff() && !(st.s != st.s);
     const float log_s = empty ? 0.0f : __builtin_logf(st.s), base = empty ? 0.0f : st.m;
-    if (threadIdx.x == 0) {
+    if (i == 0) {
         if (a.lse) a.lse[row] = empty ? -__builtin_inff() : base + log_s;
         if (a.shift) {
             a.shift[2 * row] = st.m;
@@ -205,11 +206,10 @@ __device__ __forceinline__ void finish_row(const LogprobArgs &a, size_t row, Sta
         }
         if (a.entropy) a.entropy[row] = empty ? 0.0f : log_s - st.t / st.s;
     }
-    for (int i = threadIdx.x; i < a.given; i += THREADS) {
-        if (i >= THREADS) own = given_at<TYPE>(a, row, i);
-        a.logprob[row * a.given + i] = own.real ? (own.logit - base) - log_s : 0.0f;
+    for (int g = i; g < a.given; g += WIDTH) {
+        if (g >= WIDTH) own = given_at<TYPE>(a, row, g);
+        a.logprob[row * a.given + g] = own.real ? (own.logit - base) - log_s : 0.0f;
     }
-    const int i = threadIdx.x;
     if (i < a.top) {
         const bool real = list[i] > none_key() && log_s == log_s;
         a.top_index[row * a.top + i] = real ? (int32_t)index_of(list[i]) : -1;
@@ -217,137 +217,74 @@ __device__ __forceinline__ void finish_row(const LogprobArgs &a, size_t row, Sta
     }
 }
 
-// A workgroup takes one part of a row (per_part logits, whole chunks; parts = 1: the row) chunk by chunk.  Each thread keeps statistics of its
-// own logits; alternatives are looked for where some thread's largest logit is above the last of the list: the logits above it, or, where
-// many threads have some, those not below the top-th of the groups' largest.
-template <int TYPE, bool TOP, bool ENTROPY>
+// `raw` (largest m) taken into a thread's statistics.
+template <int TYPE, int HELD, bool ENTROPY> __device__ __forceinline__ void take(Stats &st, const Real8<TYPE> (&raw)[HELD], float m)
+{
+    if (m > st.m) st = rescaled(st, m);
+    if (__builtin_fabsf(st.m) < 1024.0f) {
+        // in powers of 2, one operation for the difference: exp(l - m) = 2^(l c - m c) with c = log2 e.  m c rounds; what it lost (below
+        // 2^-13 here) is one factor of all terms, 1 - lost log 2 to 2^-27
+        const float mc = st.m * LOG2E, lost = __builtin_fmaf(st.m, LOG2E, -mc);
+        float s[2] = {0.0f, 0.0f}, t[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < HELD; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float d = __builtin_fmaf(raw[i][j], LOG2E, -mc), e = __builtin_amdgcn_exp2f(d);
+                s[j & 1] += e;
+                if (ENTROPY) t[j & 1] = __builtin_fmaf(e, fmaxf(d, -300.0f), t[j & 1]);      // (e = 0 from there on, also for -inf)
+            }
+        const float some = s[0] + s[1], back = 1.0f - lost * LN2;
+        st.s = __builtin_fmaf(some, back, st.s);
+        if (ENTROPY) st.t = __builtin_fmaf((t[0] + t[1] - lost * some) * LN2, back, st.t);
+    } else {                                                // (only masks so far, or logits of an unusual size)
+        const float base = st.m == -__builtin_inff() ? 0.0f : st.m;
+#pragma unroll
+        for (int i = 0; i < HELD; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float d = raw[i][j] - base, e = exp_of(d);
+                st.s += e;
+                if (ENTROPY) st.t = __builtin_fmaf(e, fmaxf(d, -200.0f), st.t);
+            }
+    }
+}
+
+// Wide rows whose alternatives nobody asks for.  A workgroup takes one part of a row (per_part logits; parts = 1: the row) chunk by chunk, the next chunk's
+// loads ahead of the sums; each thread keeps statistics of its own logits.  What bounds it: the memory (4096 x 32000 bfloat16 with entropy 51 us, 5.1 TB/s),
+// for few rows two launches and their trips to memory (1 x 128000 6.7 us).
+template <int TYPE, bool ENTROPY>
 __global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobArgs a)
 {
     typedef real_t<TYPE> T;
-    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     __shared__ Stats wave_stats[THREADS / 64];
-    TopLds &top = *reinterpret_cast<TopLds *>(smem);
     const int tid = threadIdx.x;
     const size_t row = blockIdx.x / a.parts;
     const int part = blockIdx.x % a.parts;
     const int first = part * a.per_part, last = min(first + a.per_part, a.vocab);
     const T *l = static_cast<const T *>(a.logits) + row * (size_t)a.stride;
-    float floor_value = -3.402823466e38f;           // what a logit has to reach (-inf is no alternative)
-    int waiting = 0;                                // candidates found
-    if (TOP && tid == 0) top.count = 0;             // (behind a barrier before it is used)
     const Given own = a.parts == 1 ? given_at<TYPE>(a, row, tid) : Given{false, 0.0f};
     Stats st{-__builtin_inff(), 0.0f, 0.0f};
     Real8<TYPE> next[STEPS];
-    auto load_chunk = [&](Real8<TYPE> *v, int c0) {
+    auto load_chunk = [&](int c0) {
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
             const int c = c0 + 8 * (tid + i * THREADS);
-            v[i].load(l + c, last - c, -__builtin_inff());
+            next[i].load(l + c, last - c, -__builtin_inff());
         }
     };
-    load_chunk(next, first);
+    load_chunk(first);
     for (int c0 = first; c0 < last; c0 += CHUNK) {
         float m = -__builtin_inff();
-        {
-            Real8<TYPE> raw[STEPS];
+        Real8<TYPE> raw[STEPS];
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) raw[i] = next[i];
-            if (c0 + CHUNK < last) load_chunk(next, c0 + CHUNK);
+        for (int i = 0; i < STEPS; ++i) raw[i] = next[i];
+        if (c0 + CHUNK < last) load_chunk(c0 + CHUNK);
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i)
+        for (int i = 0; i < STEPS; ++i)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) m = fmaxf(m, raw[i][j]);
-            if (m > st.m) st = rescaled(st, m);
-            if (__builtin_fabsf(st.m) < 1024.0f) {
-                // in powers of 2, one operation for the difference: exp(l - m) = 2^(l c - m c) with c = log2 e.  m c rounds; what it lost (below
-                // 2^-13 here) is one factor of all terms, 1 - lost log 2 to 2^-27
-                const float mc = st.m * LOG2E, lost = __builtin_fmaf(st.m, LOG2E, -mc);
-                float s[2] = {0.0f, 0.0f}, t[2] = {0.0f, 0.0f};
-#pragma unroll
-                for (int i = 0; i < STEPS; ++i)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float d = __builtin_fmaf(raw[i][j], LOG2E, -mc), e = __builtin_amdgcn_exp2f(d);
-                        s[j & 1] += e;
-                        if (ENTROPY) t[j & 1] = __builtin_fmaf(e, fmaxf(d, -300.0f), t[j & 1]);      // (e = 0 from there on, also for -inf)
-                    }
-                const float some = s[0] + s[1], back = 1.0f - lost * LN2;
-                st.s = __builtin_fmaf(some, back, st.s);
-                if (ENTROPY) st.t = __builtin_fmaf((t[0] + t[1] - lost * some) * LN2, back, st.t);
-            } else {                                                // (only masks so far, or logits of an unusual size)
-                const float base = st.m == -__builtin_inff() ? 0.0f : st.m;
-#pragma unroll
-                for (int i = 0; i < STEPS; ++i)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float d = raw[i][j] - base, e = exp_of(d);
-                        st.s += e;
-                        if (ENTROPY) st.t = __builtin_fmaf(e, fmaxf(d, -200.0f), st.t);
-                    }
-            }
-        }
-        if (TOP) {
-            const int over = __syncthreads_count(m >= floor_value);
-            if (over == 0) continue;
-            const bool many = over > GROUP_LANES * a.top;
-            if (many) {
-                uint32_t most = (uint32_t)(key_of(m, 0) >> 32);
-#pragma unroll
-                for (int d = 1; d < GROUP_LANES; d <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d, 64));
-                if (tid % GROUP_LANES == 0) top.short_group[tid / GROUP_LANES] = short_key(most, tid / GROUP_LANES);
-                __syncthreads();
-                floor_value = fmaxf(floor_value, value_of((key_t)short_rank(top.short_group, a.top) << 32));
-            }
-            // one bit per logit; the few threads that have one read theirs once more, from the cache (registers for all would cost more)
-            static_assert(8 * STEPS == 32, "");
-            uint32_t taken = 0;
-            if (m >= floor_value) {
-                Real8<TYPE> again[STEPS];
-                load_chunk(again, c0);
-#pragma unroll
-                for (int i = 0; i < STEPS; ++i)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) taken |= again[i][j] >= floor_value ? 1u << (8 * i + j) : 0;
-            }
-            auto key_at = [&](int bit) {
-                const uint32_t index = (uint32_t)(c0 + 8 * (tid + (bit >> 3) * THREADS) + (bit & 7));
-                return key_of((float)l[index], index);
-            };
-            int at = taken ? atomicAdd(&top.count, __builtin_popcount(taken)) : 0;
-            __syncthreads();
-            const int before = waiting;
-            waiting = top.count;
-            if (waiting - before <= a.top * GROUP_LANES * 8 * STEPS) {
-                for (; taken; taken &= taken - 1) top.found[at++] = key_at(__builtin_ctz(taken));
-            } else {
-                // so many equal logits that they overflow the list: with their indices for order, as many as one list's worth are left
-                key_t best = 0;
-                for (uint32_t bits = taken; bits; bits &= bits - 1) best = max(best, key_at(__builtin_ctz(bits)));
-                const key_t least = group_threshold(top, best, a.top);
-                if (tid == 0) top.count = before;
-                __syncthreads();
-                for (; taken; taken &= taken - 1) {
-                    const key_t k = key_at(__builtin_ctz(taken));
-                    if (k >= least) top.found[atomicAdd(&top.count, 1)] = k;
-                }
-                __syncthreads();
-                waiting = top.count;
-            }
-            // (at least `top` of those found reach the floor: of what follows, only what is above it)
-            if (many) floor_value = above(floor_value);
-            if (waiting > KEPT) {
-                __syncthreads();
-                select_top(top, waiting, a.top);
-                waiting = a.top;
-                if (tid < a.top) top.found[tid] = top.list[tid];
-                if (tid == 0) top.count = a.top;
-                floor_value = fmaxf(floor_value, above(value_of(top.list[a.top - 1])));
-            }
-        }
-    }
-    if (TOP) {
-        __syncthreads();
-        select_top(top, waiting, a.top);
+            for (int j = 0; j < 8; ++j) m = fmaxf(m, raw[i][j]);
+        take<TYPE, STEPS, ENTROPY>(st, raw, m);
     }
     st = wave_merged(st);
     if ((tid & 63) == 0) wave_stats[tid >> 6] = st;
@@ -364,15 +301,12 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobArgs a)
         }
         st = {m, s, t};
     }
-    if (a.parts == 1) {
-        finish_row<TYPE>(a, row, st, top.list, own);
-    } else {
-        if (tid == 0) a.part_stats[blockIdx.x] = st;
-        if (TOP && tid < a.top) a.part_top[(size_t)blockIdx.x * a.top + tid] = top.list[tid];
-    }
+    if (a.parts == 1) finish_row<TYPE>(a, row, st, nullptr, own);
+    else if (tid == 0) a.part_stats[blockIdx.x] = st;
 }
 
-// The parts of a row joined, in their order.  Each part's list is in order, so the first keys tell which lists can hold an alternative.
+// The parts of a row joined, in their order.  Each part's list is in order: the top-th of 64 of the lists' first keys
+// bounds the alternatives from below.
 template <int TYPE>
 __global__ __launch_bounds__(THREADS) void logprobs_join_kernel(LogprobArgs a)
 {
@@ -380,12 +314,13 @@ __global__ __launch_bounds__(THREADS) void logprobs_join_kernel(LogprobArgs a)
     TopLds &top = *reinterpret_cast<TopLds *>(smem);
     const int tid = threadIdx.x, n = a.parts * a.top;
     const size_t row = blockIdx.x;
-    constexpr int MOST = 64 * 32 / THREADS;
+    constexpr int MOST = MOST_PARTS * MOST_TOP / THREADS;
     Stats st{-__builtin_inff(), 0.0f, 0.0f};
     if ((tid & 63) < a.parts) st = a.part_stats[row * a.parts + (tid & 63)];      // (every wave joins them all)
     key_t first = none_key(), mine[MOST];
     if (a.top) {
-        if (tid < a.parts) first = a.part_top[row * n + (size_t)tid * a.top];
+        const int list = tid % a.parts, at = tid / a.parts;
+        if (tid < 64 && at < min(a.top, 64 / a.parts)) first = a.part_top[row * n + (size_t)list * a.top + at];
 #pragma unroll
         for (int i = 0; i < MOST; ++i) {
             const int at = tid + i * THREADS;
@@ -408,120 +343,170 @@ __global__ __launch_bounds__(THREADS) void logprobs_join_kernel(LogprobArgs a)
     finish_row<TYPE>(a, row, st, top.list, own);
 }
 
-// Narrow rows (at most 64 * 8 * HELD logits): a wave each, in registers, without barriers.  Alternatives: the logits not below the top-th of the lanes'
-// largest, ranked by counting; where equal ones overflow the list, the largest is taken `top` times.
-template <int TYPE, int HELD>
-__global__ __launch_bounds__(THREADS) void logprobs_narrow_kernel(LogprobArgs a, int rows)
+// Rows whose alternatives are wanted, and narrow ones: a wave takes a part of a row (parts = 1: the row), 64 * 8 * HELD logits at a time in registers
+// (LOOP: more than once, the next ones' loads ahead), without barriers.  Each lane keeps statistics and the largest of its own logits; the top-th of the
+// lanes' largest bounds the alternatives from below, and only a few more logits reach it (64 log 2 = 44 of any number in random order for top = 32).  Lanes
+// that hold one put their logits side by side in LDS, all lanes look through them, and what reaches the bound waits in a list, whose best are ranked by
+// counting once it is full and at the end.
+// What bounds it: a short row's chain of latencies (1 x 1000 bfloat16 3.5 us without alternatives, 5.7 with 20); on long ones the search's instructions beside
+// the exponents' (4096 x 32000 bfloat16, 20 alternatives, 66 us, 4.0 TB/s; a workgroup per row, whose barriers every chunk waits for, 90).
+template <int TYPE, int HELD, bool LOOP>
+__global__ __launch_bounds__(THREADS) void logprobs_wave_kernel(LogprobArgs a, int tasks)
 {
     typedef real_t<TYPE> T;
-    constexpr int LIST = 128;
-    __shared__ __attribute__((aligned(16))) uint32_t lane_keys[THREADS / 64][64];
-    __shared__ key_t lists[THREADS / 64][LIST];
+    constexpr int WAVES = THREADS / 64, LIST = 256, OWN = 8 * HELD, SPAN = 64 * OWN;
+    constexpr int PITCH = OWN + 16 / (int)sizeof(T);                                    // (16 bytes more: lanes in other banks)
+    __shared__ __attribute__((aligned(16))) uint32_t lane_keys[WAVES][64];
+    __shared__ __attribute__((aligned(16))) key_t lists[WAVES][LIST];
+    __shared__ __attribute__((aligned(16))) T held[WAVES][64][PITCH];
+    __shared__ uint8_t holders[WAVES][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const size_t row = (size_t)blockIdx.x * (THREADS / 64) + wave;
-    if (row >= (size_t)rows) return;
+    const int task = blockIdx.x * WAVES + wave;
+    if (task >= tasks) return;
+    const size_t row = LOOP ? task / a.parts : task;
+    const int first = LOOP ? (task - (int)row * a.parts) * a.per_part : 0, last = LOOP ? min(first + a.per_part, a.vocab) : a.vocab;
     const T *l = static_cast<const T *>(a.logits) + row * (size_t)a.stride;
-    Real8<TYPE> raw[HELD];
+    Real8<TYPE> next[HELD];
+    auto load = [&](int c0) {
 #pragma unroll
-    for (int i = 0; i < HELD; ++i) {
-        const int c = 8 * (lane + 64 * i);
-        raw[i].load(l + c, a.vocab - c, -__builtin_inff());
-    }
-    Given own = given_at<TYPE>(a, row, lane);
-    float m = -__builtin_inff();
-#pragma unroll
-    for (int i = 0; i < HELD; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) m = fmaxf(m, raw[i][j]);
-    const float lane_most = m;
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
-    const float base = m == -__builtin_inff() ? 0.0f : m;
-    float s = 0.0f, t = 0.0f;
-#pragma unroll
-    for (int i = 0; i < HELD; ++i) {
-        if (512 * i >= a.vocab) break;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float d = raw[i][j] - base, e = exp_of(d);
-            s += e;
-            t = __builtin_fmaf(e, fmaxf(d, -200.0f), t);        // (e = 0 from there on, also for -inf)
+        for (int i = 0; i < HELD; ++i) {
+            const int c = c0 + 8 * (lane + 64 * i);
+            next[i].load(l + c, last - c, -__builtin_inff());
         }
-    }
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-        s += __shfl_xor(s, d, 64);
-        t += __shfl_xor(t, d, 64);
-    }
-    const bool empty = m == -__builtin_inff() && s == s;
-    const float log_s = empty ? 0.0f : __builtin_logf(s);
-    if (lane == 0) {
-        if (a.lse) a.lse[row] = empty ? -__builtin_inff() : base + log_s;
-        if (a.shift) {
-            a.shift[2 * row] = m;
-            a.shift[2 * row + 1] = log_s;
-        }
-        if (a.entropy) a.entropy[row] = empty ? 0.0f : log_s - t / s;
-    }
-    for (int i = lane; i < a.given; i += 64) {
-        if (i >= 64) own = given_at<TYPE>(a, row, i);
-        a.logprob[row * a.given + i] = own.real ? (own.logit - base) - log_s : 0.0f;
-    }
-    if (a.top == 0) return;
-    auto put = [&](int rank, bool real, key_t k) {
-        a.top_index[row * a.top + rank] = real ? (int32_t)index_of(k) : -1;
-        a.top_logprob[row * a.top + rank] = real ? (value_of(k) - base) - log_s : log_s == log_s ? -__builtin_inff() : log_s;
     };
-    if (log_s != log_s) {
-        if (lane < a.top) put(lane, false, 0);
-        return;
-    }
-    lane_keys[wave][lane] = short_key((uint32_t)(key_of(lane_most, 0) >> 32), lane);
-    wave_fence();
-    const float floor_value = fmaxf(-3.402823466e38f, value_of((key_t)short_rank(lane_keys[wave], a.top) << 32));
-    uint32_t taken = 0;
-#pragma unroll
-    for (int i = 0; i < HELD; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) taken |= raw[i][j] >= floor_value ? 1u << (8 * i + j) : 0;
-    auto key_at = [&](int bit) {
-        const uint32_t index = (uint32_t)(8 * (lane + 64 * (bit >> 3)) + (bit & 7));
-        return key_of((float)l[index], index);
+    load(first);
+    Given own = !LOOP || a.parts == 1 ? given_at<TYPE>(a, row, lane) : Given{false, 0.0f};
+    Stats st{-__builtin_inff(), 0.0f, 0.0f};
+    key_t *const list = lists[wave];
+    int n = 0;                                      // candidates in the list
+    float bound = -3.402823466e38f, floor_value = bound;       // what the alternatives reach (-inf is none); what a logit has to reach to be looked at
+    auto below = [](unsigned long long mask) { return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)); };
+    auto raise_bound = [&]() {
+        lane_keys[wave][lane] = short_key((uint32_t)(key_of(st.m, 0) >> 32), lane);
+        wave_fence();
+        bound = fmaxf(bound, value_of((key_t)short_rank(lane_keys[wave], a.top) << 32));
+        floor_value = fmaxf(floor_value, bound);
+        wave_fence();
     };
-    int at = __builtin_popcount(taken);
-    const int mine = at;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(at, d, 64);
-        at += lane >= d ? o : 0;
-    }
-    const int n = __builtin_amdgcn_readlane(at, 63);
-    if (n > LIST) {
-        key_t last = ~(key_t)0;
-        for (int rank = 0; rank < a.top; ++rank) {
-            key_t best = 0;
-            for (uint32_t bits = taken; bits; bits &= bits - 1) {
-                const key_t k = key_at(__builtin_ctz(bits));
-                best = k < last && k > best ? k : best;
-            }
-#pragma unroll
-            for (int d = 32; d > 0; d >>= 1) best = max(best, (key_t)__shfl_xor((long long)best, d, 64));
-            last = best;
-            if (lane == 0) put(rank, best != 0, best);
+    // the list's best in order: keys differ, so every rank is taken once
+    auto rank_list = [&]() {
+        int kept = n > 64 ? 0 : n;
+        if (n > 64) raise_bound();                  // (a long list is thinned out first)
+        for (int i = 0; i < n && n > 64; i += 64) {
+            const key_t k = i + lane < n ? list[i + lane] : 0;
+            const bool keep = i + lane < n && value_of(k) >= bound;
+            const unsigned long long mask = __ballot(keep);
+            wave_fence();
+            if (keep) list[kept + below(mask)] = k;
+            kept += __builtin_popcountll(mask);
+            wave_fence();
         }
-        return;
-    }
-    key_t *list = lists[wave];
-    for (at -= mine; taken; taken &= taken - 1) list[at++] = key_at(__builtin_ctz(taken));
-    wave_fence();
-    for (int i = lane; i < n; i += 64) {
-        const key_t k = list[i];
-        int rank = 0;
+        key_t k[LIST / 64];
+        int rank[LIST / 64];
+#pragma unroll
+        for (int i = 0; i < LIST / 64; ++i) {
+            if (64 * i >= kept) break;
+            k[i] = lane + 64 * i < kept ? list[lane + 64 * i] : 0;
+            rank[i] = 0;
 #pragma unroll 8
-        for (int j = 0; j < n; ++j) rank += list[j] > k ? 1 : 0;
-        if (rank < a.top) put(rank, true, k);
+            for (int j = 0; j < kept; ++j) rank[i] += list[j] > k[i] ? 1 : 0;
+        }
+        wave_fence();
+#pragma unroll
+        for (int i = 0; i < LIST / 64; ++i) {
+            if (64 * i >= kept) break;
+            if (lane + 64 * i < kept && rank[i] < a.top) list[rank[i]] = k[i];
+        }
+        n = min(kept, a.top);
+        wave_fence();
+    };
+    for (int c0 = first; c0 < last; c0 += SPAN) {
+        Real8<TYPE> raw[HELD];
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) raw[i] = next[i];
+        if (LOOP && c0 + SPAN < last) load(c0 + SPAN);
+        float m = -__builtin_inff();
+#pragma unroll
+        for (int i = 0; i < HELD; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m = fmaxf(m, raw[i][j]);
+        take<TYPE, HELD, true>(st, raw, m);
+        if (a.top == 0) continue;
+        unsigned long long over = __ballot(m >= floor_value);
+        if (over == 0) continue;
+        const bool many = __builtin_popcountll(over) > 8;       // (fewer are looked through sooner than the bound is found anew)
+        if (many) {
+            raise_bound();
+            over = __ballot(m >= floor_value);
+        }
+        if (m >= floor_value) {
+            const int slot = below(over);
+            holders[wave][slot] = (uint8_t)lane;
+#pragma unroll
+            for (int i = 0; i < HELD; ++i)
+#pragma unroll
+                for (int q = 0; q < Real8<TYPE>::QUADS; ++q)
+                    reinterpret_cast<uint4 *>(held[wave][slot])[i * Real8<TYPE>::QUADS + q] = make_uint4(raw[i].quad[q][0], raw[i].quad[q][1], raw[i].quad[q][2],
+                                                                                                          raw[i].quad[q][3]);
+        }
+        if (many) {                                 // each lane by itself
+            uint32_t taken = 0;
+#pragma unroll
+            for (int i = 0; i < HELD; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) taken |= raw[i][j] >= floor_value ? 1u << (8 * i + j) : 0;
+            int at = __builtin_popcount(taken);
+            const int mine = at;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int o = __shfl_up(at, d, 64);
+                at += lane >= d ? o : 0;
+            }
+            const int found = __builtin_amdgcn_readlane(at, 63);
+            if (n + found <= LIST) {
+                const T *const values = held[wave][below(over)];
+                wave_fence();
+                for (at += n - mine; taken; taken &= taken - 1) {
+                    const int bit = __builtin_ctz(taken);
+                    list[at++] = key_of((float)values[bit], (uint32_t)(c0 + 8 * (lane + 64 * (bit >> 3)) + (bit & 7)));
+                }
+                n += found;
+                continue;
+            }
+        }
+        // few of them, or so many that they overflow the list: one after the other
+        wave_fence();
+        key_t least = 0;                            // (what a key has to be above once the list was ranked)
+        auto rank_now = [&]() {
+            rank_list();
+            if (n == a.top) least = list[a.top - 1];
+        };
+        if (n > LIST - 64) rank_now();
+        const int entries = __builtin_popcountll(over) * OWN;
+        for (int e = lane; e - lane < entries; e += 64) {
+            const int slot = min(e / OWN, 63), at = e % OWN;
+            const float v = e < entries ? (float)held[wave][slot][at] : -__builtin_inff();
+            const key_t k = key_of(v, (uint32_t)(c0 + 8 * (holders[wave][slot] + 64 * (at >> 3)) + (at & 7)));
+            const bool taken = v >= floor_value && k > least;
+            const unsigned long long mask = __ballot(taken);
+            if (taken) list[n + below(mask)] = k;
+            n += __builtin_popcountll(mask);
+            if (n > LIST - 64) rank_now();
+        }
+        wave_fence();
+        // (of what follows, only what is above the last of `top` in the list)
+        if (least) floor_value = fmaxf(floor_value, above(value_of(least)));
     }
-    if (lane >= n && lane < a.top) put(lane, false, 0);
+    if (a.top) rank_list();
+    st = wave_merged(st);
+    if (LOOP && a.parts > 1) {
+        if (lane == 0) a.part_stats[task] = st;
+        if (lane < a.top) a.part_top[(size_t)task * a.top + lane] = lane < n ? list[lane] : none_key();
+        return;
+    }
+    if (lane < a.top && lane >= n) list[lane] = none_key();
+    wave_fence();
+    finish_row<TYPE, 64>(a, row, st, list, own);
 }
 
 struct LogprobGradArgs {
@@ -585,22 +570,21 @@ __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(LogprobGradArgs 
     }
 }
 
-// Parts of a row: few rows are spread over the chip.
-int logprobs_parts(int rows, int vocab)
+// Parts of a row: few rows are spread over the chip, workgroups (no alternatives) or waves.  Fewer waves leave SIMDs idle, more repeat each part's search and
+// are joined in a second launch: 1500 bfloat16 rows of 32000, 20 alternatives, 40 us in two parts, 47 in one; 512 rows 22 in eight, 25 in four, 30 in two.
+int logprobs_parts(int rows, int vocab, int top)
 {
     const int longest = (vocab + 2047) / 2048;
-    if (vocab <= CHUNK) return 1;
-    return std::max(1, std::min({longest, 512 / std::max(rows, 1), 64}));
+    if (vocab <= (top ? 64 * 8 * STEPS : CHUNK)) return 1;
+    return std::max(1, std::min({longest, (top ? 4096 : 512) / std::max(rows, 1), MOST_PARTS}));
 }
 int logprobs_per_part(int vocab, int parts) { return ((vocab + parts - 1) / parts + 7) / 8 * 8; }
-
-size_t top_lds(int top, int keys) { return top ? sizeof(TopLds) + (size_t)keys * sizeof(key_t) : 0; }
 
 }  // namespace
 
 size_t logprobs_workspace_bytes(int rows, int vocab, int top)
 {
-    const int parts = logprobs_parts(rows, vocab);
+    const int parts = logprobs_parts(rows, vocab, top);
     return parts == 1 ? 0 : (size_t)rows * parts * (16 + 8 * (size_t)top);
 }
 
@@ -608,29 +592,23 @@ xnor_status launch_logprobs(const void *logits, long long stride, const void *to
                             int32_t *top_index, float *top_logprob, void *workspace, int rows, int vocab, int given, int top, int type,
                             hipStream_t stream)
 {
-    const int parts = logprobs_parts(rows, vocab);
+    const int parts = logprobs_parts(rows, vocab, top);
     const LogprobArgs a{logits, tokens, logprob, lse, shift, entropy, top_index, top_logprob,
                         reinterpret_cast<Stats *>(static_cast<char *>(workspace) + (size_t)rows * parts * top * 8), static_cast<key_t *>(workspace),
                         stride, vocab, given, top, token_bytes, parts, logprobs_per_part(vocab, parts)};
-    const dim3 grid((unsigned)(rows * parts)), threads(THREADS);
-    if (vocab <= 64 * 8 * STEPS) {
-        const dim3 fours((unsigned)((rows + THREADS / 64 - 1) / (THREADS / 64)));
-        by_type(type, [&](auto t) {
-            if (vocab <= 512) logprobs_narrow_kernel<t(), 1><<<fours, threads, 0, stream>>>(a, rows);
-            else logprobs_narrow_kernel<t(), STEPS><<<fours, threads, 0, stream>>>(a, rows);
-        });
-        return hip_status(hipGetLastError());
-    }
+    const int tasks = rows * parts;
+    const dim3 threads(THREADS), all((unsigned)tasks), fours((unsigned)((tasks + THREADS / 64 - 1) / (THREADS / 64)));
     by_type(type, [&](auto t) {
-        const size_t lds = top_lds(top, KEPT + top * GROUP_LANES * 8 * STEPS);
-        if (top && entropy) logprobs_kernel<t(), true, true><<<grid, threads, lds, stream>>>(a);
-        else if (top) logprobs_kernel<t(), true, false><<<grid, threads, lds, stream>>>(a);
-        else if (entropy) logprobs_kernel<t(), false, true><<<grid, threads, 0, stream>>>(a);
-        else logprobs_kernel<t(), false, false><<<grid, threads, 0, stream>>>(a);
+        if (vocab <= 512) logprobs_wave_kernel<t(), 1, false><<<fours, threads, 0, stream>>>(a, tasks);
+        else if (vocab <= 64 * 8 * STEPS) logprobs_wave_kernel<t(), STEPS, false><<<fours, threads, 0, stream>>>(a, tasks);
+        else if (top) logprobs_wave_kernel<t(), STEPS, true><<<fours, threads, 0, stream>>>(a, tasks);
+        else if (entropy) logprobs_kernel<t(), true><<<all, threads, 0, stream>>>(a);
+        else logprobs_kernel<t(), false><<<all, threads, 0, stream>>>(a);
     });
     if (xnor_status e = hip_status(hipGetLastError())) return e;
     if (parts == 1) return XNOR_OK;
-    by_type(type, [&](auto t) { logprobs_join_kernel<t()><<<dim3((unsigned)rows), threads, top_lds(top, top * parts), stream>>>(a); });
+    const size_t lds = top ? sizeof(TopLds) + (size_t)top * parts * sizeof(key_t) : 0;
+    by_type(type, [&](auto t) { logprobs_join_kernel<t()><<<dim3((unsigned)rows), threads, lds, stream>>>(a); });
     return hip_status(hipGetLastError());
 }
 

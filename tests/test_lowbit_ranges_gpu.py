@@ -8,6 +8,7 @@ import torch
 from paper_1603_05279_amd import xnor
 from tests.lowbit_helpers import EPS32, HALF_ULP, SMALLEST, TYPES, assert_within, filled, generator, normal
 from tests.test_logprobs_gpu import check as check_logprobs
+from tests.test_logprobs_gpu import run as run_logprobs
 from tests.test_w4_linear_gpu import check as check_product
 from tests.test_w4_linear_gpu import make, product, scratch
 
@@ -81,6 +82,27 @@ def test_widths_of_logits(t, vocab):
         l[rows // 3, : vocab // 2] = 1.0                                    # (and one of ties)
         check_logprobs(l, torch.randint(-1, vocab + 1, (rows, 2), generator=gen), 20)
         check_logprobs(l, torch.randint(0, vocab, (rows, 1), generator=gen, dtype=torch.int32), 0, extra=5)
+
+
+@pytest.mark.parametrize("t,vocab", [("bf16", 20003), ("f32", 9000)])
+def test_many_long_rows_of_every_order(t, vocab):
+    """Enough rows that none is shared out: alternatives are found over many chunks, of random, rising, falling, equal, masked and lopsided rows."""
+    gen = generator(vocab)
+    at = torch.arange(vocab)
+    lowest = torch.finfo(TYPES[t]).min
+    kinds = [normal(gen, vocab, scale=3), at / 64.0, -at / 64.0, torch.zeros(vocab), torch.full((vocab,), lowest), torch.full((vocab,), -math.inf),
+             torch.where(at < 5, 1.0, -math.inf), torch.where(at % 2048 < 32, at / 64.0, 0.0), torch.where(at >= vocab - 7, 2.0, lowest),
+             torch.where(torch.rand(vocab, generator=gen) < 0.99, lowest, 3.0), (at % 3).float(), torch.randint(0, 5, (vocab,), generator=gen).float()]
+    few = torch.stack(kinds).to(TYPES[t])
+    tokens = torch.randint(0, vocab, (len(kinds), 1), generator=gen)
+    times = 4200 // len(kinds)
+    for top in (1, 20, 32):
+        want = check_logprobs(few, tokens, top)
+        got = run_logprobs(few.repeat(times, 1), tokens.repeat(times, 1), top)
+        for name in ("lse", "shift", "entropy", "logprob", "top_logprob"):
+            a, b = got[name].view(times, *want[name].shape), want[name][None]
+            assert ((a == b) | ((a - b).abs() <= 2e-5 * (1 + b.abs()))).all(), name
+        assert torch.equal(got["top_index"].view(times, *want["top_index"].shape), want["top_index"].expand(times, -1, -1))
 
 
 FAR = 2 ** 31 + 24                                                          # elements between two rows: three rows pass 32 bits of elements
