@@ -63,7 +63,7 @@ __global__ __launch_bounds__(256) void w4_stage_kernel(StageArgs a)
     typedef Form<X> F;
     const Staged st(a.rows, a.in, a.group, X);
     const int lane = threadIdx.x & 63, r = lane & 15, quarter = lane >> 4;
-    const int chunk = blockIdx.x * 4 + (threadIdx.x >> 6), tile = blockIdx.y;
+    const int chunk = blockIdx.y * 4 + (threadIdx.x >> 6), tile = blockIdx.x;
     if (chunk >= st.chunks) return;
     const int row = tile * TILE + r;
     const bool real = row < a.rows;
@@ -165,7 +165,11 @@ __global__ __launch_bounds__(128 * SIDE) void w4_tiles_kernel(TileArgs a)
     const int count = a.row_blocks * a.out_blocks, per_xcd = (count + 7) / 8;
     const int id = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
     if ((int)(blockIdx.x >> 3) >= per_xcd || id >= count) return;
-    const int rb = id % a.row_blocks, ob = id / a.row_blocks;
+    // (in strips of four blocks of rows: the workgroups of an XCD read 4 blocks of rows and 8 of codes at a time, 256 KB per chunk; whole columns of blocks
+    // 544 KB.  8192 bfloat16 rows 4096 -> 8192 556 us, by columns 587)
+    constexpr int STRIP = 4;
+    const int strip = id / (STRIP * a.out_blocks), within = id - strip * STRIP * a.out_blocks, high = min(STRIP, a.row_blocks - strip * STRIP);
+    const int ob = within / high, rb = strip * STRIP + within - ob * high;
     const int otile = ob * 4 * SIDE + wo * 4, rtile = rb * BLOCK + wr * 4;
     const int parts = st.parts, steps = st.chunks * parts;
 
@@ -529,7 +533,7 @@ int w4_rows_tiles(int rows, int out)
 // which it picks one that is more than a tenth slower than the best twice.
 // w4_rows_kernel reads all rows' inputs in every workgroup, but is one launch; the others stage the rows first.  Tiles of 64 x 64 whose inputs eight waves
 // share fill the chip where few of 256 x 128 would not.  Measured by rows, by waves, by tiles: 64 bfloat16 rows 9216 -> 4096 17, 26, 138; 48 rows
-// 4096 -> 16384 21, 18, 65; 128 rows 9216 -> 4096 29, 27, 141; 600 8-bit rows 512 -> 8192 47, 26, 27; 2048 bfloat16 rows 4096 -> 8192 -, 189, 148.
+// 4096 -> 16384 21, 18, 65; 128 rows 9216 -> 4096 29, 27, 141; 600 8-bit rows 512 -> 8192 47, 26, 27; 2048 bfloat16 rows 4096 -> 8192 -, 189, 142.
 W4Kernel w4_kernel(int rows, int in, int out, int form)
 {
     int tiles;
@@ -556,7 +560,7 @@ xnor_status launch_w4_staged(W4Kernel kernel, const void *x, long long x_stride,
     const Staged st(rows, in, group, form);
     uint8_t *staged = static_cast<uint8_t *>(workspace);
     const StageArgs sa{x, x_scale, staged, x_stride, rows, in, group, x_group, x_group ? (in + x_group - 1) / x_group : 1};
-    const dim3 grid((unsigned)((st.chunks + 3) / 4), (unsigned)((rows + TILE - 1) / TILE));
+    const dim3 grid((unsigned)((rows + TILE - 1) / TILE), (unsigned)((st.chunks + 3) / 4));
     if (form == ROWS_F32) w4_stage_kernel<ROWS_F32><<<grid, dim3(256), 0, stream>>>(sa);
     else if (form == ROWS_BF16) w4_stage_kernel<ROWS_BF16><<<grid, dim3(256), 0, stream>>>(sa);
     else if (form == ROWS_F16) w4_stage_kernel<ROWS_F16><<<grid, dim3(256), 0, stream>>>(sa);

@@ -44,6 +44,22 @@ def test_staged_8_bit_products(x_group, group, rows, out, cin):
     assert_within(y, want, (-(-cin // group) + 8) * 2 * EPS32 * sums + HALF_ULP["bf16"] * want.abs() + SMALLEST["bf16"], "y")
 
 
+@pytest.mark.parametrize("out,cin", [(20, 40), (600, 200)])
+def test_a_million_rows(out, cin):
+    """More rows than 65535 tiles of 16: the first, the last and some between are looked at."""
+    gen = generator(out)
+    rows = 1_100_003
+    packed, w, top = make(gen, out, cin, 32, True)
+    x = torch.randn((rows, cin), device="cuda", generator=torch.Generator(device="cuda").manual_seed(7)).to(torch.bfloat16)
+    y = torch.empty((rows, out), dtype=torch.bfloat16, device="cuda")
+    xnor.xnor_w4_linear(x, packed.wimg, y, scratch(rows, cin, out, 32), rows, cin, out, 32)
+    some = torch.cat((torch.arange(40), torch.randint(0, rows, (40,), generator=gen), torch.arange(rows - 40, rows))).cuda()
+    x = x[some].double().cpu()
+    want = x @ w.t()
+    bound = 4 * cin * 62 * EPS32 * x.square().mean(1).sqrt()[:, None] * top[None]
+    assert_within(y[some], want, bound + HALF_ULP["bf16"] * want.abs() + SMALLEST["bf16"], "y")
+
+
 @pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("rows,out,cin", [(200, 4000, 1030), (2100, 8200, 520)])
 def test_infinities_and_nan_in_staged_rows(t, rows, out, cin):
