@@ -10,6 +10,8 @@
  *    once, to nearest even.
  *  - Rows that a call only reads may lie apart: `..._stride` is the distance of two rows in elements, at least their width.
  *    Everything else is densely packed.  Rows need no alignment of their own.
+ *  - Sizes go up to rows = 65535 * 64, in = out = 2^24, vocab = 2^30 (the backward pass of logprobs: rows * ceil(vocab / 8192) < 2^24);
+ *    beyond them and below 1 (rows: 0): XNOR_ERR_SHAPE.
  *  - rows = 0 is a call without work: XNOR_OK, nothing is launched and no pointer is looked at.
  *  - Where two kernels are enqueued, the first may be when the second reports XNOR_ERR_HIP; it writes that call's own outputs or
  *    workspace only.  A workspace's contents are undefined afterwards, and nothing in it has to be cleared before.

