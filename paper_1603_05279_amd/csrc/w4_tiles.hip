@@ -143,9 +143,10 @@ __device__ __forceinline__ void to_lds(const uint8_t *from, uint8_t *to)        
 // STEPS of 32 inputs per group.  2 * SIDE waves, each 64 outputs x 64 rows, together 64 * SIDE outputs x 128 rows.  All a chunk needs (the rows' operands,
 // codes, scales, zero points) goes straight to one of BUFFERS places in LDS, BUFFERS - 1 chunks ahead, one barrier per chunk.  Every wave issues
 // the same number of loads for a chunk, so that it can wait for its oldest chunk alone.  GROUPED: 8-bit rows with scales of groups.
-// What bounds it: issue.  A wave's chunk is 64 matrix instructions of 16 cycles and 230 others of four to five (128 widen the codes, 64 scale), which
-// overlap with another wave's by half: 2048 bfloat16 rows 4096 -> 8192, groups of 128, 138 us with the staging, 1.0 PFLOP/s (a library's product with bfloat16
-// weights 99), groups of 32 198, 8 bits 121.  Instructions of 32 x 32 results: 156, 248, 122; the next chunk's first operands read ahead of the barrier: 149.
+// What bounds it: the matrix instructions at the clock that the chip holds under them.  2048 bfloat16 rows 4096 -> 8192, groups of 128: 138 us with the staging,
+// 1.0 PFLOP/s (a library's product with bfloat16 weights 99); the same loop of matrix instructions alone takes 92, 16 cycles each at 1.43 GHz, the loads into
+// LDS add 15, the scaling 9, reading LDS 5, widening the codes nothing; launches, staging, first loads and stores are 18.  Groups of 32 198 us, 8 bits 121.
+// Instructions of 32 x 32 results: 156, 248, 122; the next chunk's first operands read ahead of the barrier: 149.
 template <int X, int STEPS, bool GROUPED, int SIDE> struct TilePlace {
     static constexpr int WAVES = 2 * SIDE, PER_CHUNK = 4 / STEPS, TB = X == ROWS_I8 ? 2048 : 4096;
     static constexpr int ROWS = 0, CODES = BLOCK * TB, SCALES = CODES + SIDE * 4096, FACTORS = 4 * PER_CHUNK * 64;      // of four tiles
