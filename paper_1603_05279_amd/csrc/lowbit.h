@@ -23,8 +23,12 @@ xnor_status launch_w4_linear_q8(const int8_t *q, const float *x_scale, const voi
                                 int x_group, int type, hipStream_t stream);
 // products (form: the rows' xnor_dtype, or 3 for 8 bits): w4_rows_kernel, or the kernels of w4_tiles.hip on staged rows
 enum W4Kernel { W4_ROWS, W4_WAVES, W4_TILES };
-W4Kernel w4_kernel(int rows, int in, int out, int form);
-int w4_rows_tiles(int rows, int out);       // tiles of 16 outputs per workgroup of w4_rows_kernel
+struct W4Choice {
+    W4Kernel kernel;
+    int tiles;              // of 16 outputs per workgroup of w4_rows_kernel
+    double time;            // us, expected
+};
+W4Choice w4_choice(int rows, int in, int out, int group, int form);
 size_t w4_staged_bytes(int rows, int in, int out, int group);
 xnor_status launch_w4_staged(W4Kernel kernel, const void *x, long long x_stride, const float *x_scale, const void *wimg, void *y, void *workspace, int rows,
                              int in, int out, int group, int x_group, int form, int type, hipStream_t stream);

@@ -230,19 +230,18 @@ template <int X, bool GROUPED, int STEPS, int TILES, int DEPTH> void launch_rows
 }
 // (chunks ahead: two of one or two tiles, but for float32 rows and groups of 32, which fill the registers.  Four of one tile 25.5 us for 8 8-bit rows
 // 4096 -> 32000, two 24; sixteen waves 30)
-template <int X, bool GROUPED, int STEPS> void launch_steps(const W4Args &a, hipStream_t stream)
+template <int X, bool GROUPED, int STEPS> void launch_steps(const W4Args &a, int tiles, hipStream_t stream)
 {
     constexpr int TWO = X == ROWS_F32 || STEPS == 1 ? 1 : 2;
-    const int tiles = w4_rows_tiles(a.rows, a.out);
     if (tiles == 4) launch_rows<X, GROUPED, STEPS, 4, 1>(a, stream);
     else if (tiles == 2) launch_rows<X, GROUPED, STEPS, 2, TWO>(a, stream);
     else launch_rows<X, GROUPED, STEPS, 1, TWO>(a, stream);
 }
-template <int X, bool GROUPED> xnor_status launch_groups(const W4Args &a, int group, hipStream_t stream)
+template <int X, bool GROUPED> xnor_status launch_groups(const W4Args &a, int group, int tiles, hipStream_t stream)
 {
-    if (group == 32) launch_steps<X, GROUPED, 1>(a, stream);
-    else if (group == 64) launch_steps<X, GROUPED, 2>(a, stream);
-    else launch_steps<X, GROUPED, 4>(a, stream);
+    if (group == 32) launch_steps<X, GROUPED, 1>(a, tiles, stream);
+    else if (group == 64) launch_steps<X, GROUPED, 2>(a, tiles, stream);
+    else launch_steps<X, GROUPED, 4>(a, tiles, stream);
     return hip_status(hipGetLastError());
 }
 
@@ -275,22 +274,23 @@ size_t w4_linear_workspace_bytes(int rows, int in, int out, int group) { return 
 xnor_status launch_w4_linear(const void *x, long long x_stride, const void *wimg, void *y, void *workspace, int rows, int in, int out, int group, int type,
                              hipStream_t stream)
 {
-    const W4Kernel kernel = w4_kernel(rows, in, out, type);
-    if (kernel != W4_ROWS) return launch_w4_staged(kernel, x, x_stride, nullptr, wimg, y, workspace, rows, in, out, group, 0, type, type, stream);
+    const W4Choice choice = w4_choice(rows, in, out, group, type);
+    if (choice.kernel != W4_ROWS) return launch_w4_staged(choice.kernel, x, x_stride, nullptr, wimg, y, workspace, rows, in, out, group, 0, type, type, stream);
     const W4Args a{x, nullptr, static_cast<const uint8_t *>(wimg), y, x_stride, rows, in, out, 0, 0, type};
-    if (type == XNOR_F32) return launch_groups<ROWS_F32, false>(a, group, stream);
-    if (type == XNOR_BF16) return launch_groups<ROWS_BF16, false>(a, group, stream);
-    return launch_groups<ROWS_F16, false>(a, group, stream);
+    if (type == XNOR_F32) return launch_groups<ROWS_F32, false>(a, group, choice.tiles, stream);
+    if (type == XNOR_BF16) return launch_groups<ROWS_BF16, false>(a, group, choice.tiles, stream);
+    return launch_groups<ROWS_F16, false>(a, group, choice.tiles, stream);
 }
 
 xnor_status launch_w4_linear_q8(const int8_t *q, const float *x_scale, const void *wimg, void *y, void *workspace, int rows, int in, int out, int group,
                                 int x_group, int type, hipStream_t stream)
 {
-    const W4Kernel kernel = w4_kernel(rows, in, out, ROWS_I8);
-    if (kernel != W4_ROWS) return launch_w4_staged(kernel, q, in, x_scale, wimg, y, workspace, rows, in, out, group, x_group, ROWS_I8, type, stream);
+    const W4Choice choice = w4_choice(rows, in, out, group, ROWS_I8);
+    if (choice.kernel != W4_ROWS)
+        return launch_w4_staged(choice.kernel, q, in, x_scale, wimg, y, workspace, rows, in, out, group, x_group, ROWS_I8, type, stream);
     const W4Args a{q, x_scale, static_cast<const uint8_t *>(wimg), y, in, rows, in, out, x_group ? (in + x_group - 1) / x_group : 0,
                    x_group ? __builtin_ctz(x_group / group) : 0, type};
-    return x_group ? launch_groups<ROWS_I8, true>(a, group, stream) : launch_groups<ROWS_I8, false>(a, group, stream);
+    return x_group ? launch_groups<ROWS_I8, true>(a, group, choice.tiles, stream) : launch_groups<ROWS_I8, false>(a, group, choice.tiles, stream);
 }
 
 }  // namespace xnor

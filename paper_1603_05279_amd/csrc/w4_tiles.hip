@@ -504,60 +504,47 @@ template <int X, bool GROUPED> xnor_status launch_tiles(const TileArgs &a, int g
 
 }  // namespace
 
-namespace {
 // Rounds of a workgroup per CU.
-double rounds(int out, int outs, int rows, int height)
+static double rounds(int out, int outs, int rows, int height)
 {
     return std::ceil((double)((out + outs - 1) / outs) * ((rows + height - 1) / height) / 256);
 }
-// us per chunk of 128 inputs and round of w4_rows_kernel, by tiles
-constexpr struct { int tiles; double cost; } BY_TILES[] = {{1, 0.11}, {2, 0.155}, {4, 0.2}};
-double rows_cost(int rows, int out, int *tiles)
-{
-    double best = 0;
-    for (const auto &t : BY_TILES) {
-        const double cost = t.cost * rounds(out, 16 * t.tiles, rows, 16);
-        if (best == 0 || cost < best) {
-            best = cost;
-            *tiles = t.tiles;
-        }
-    }
-    return best;
-}
-}  // namespace
 
-// More tiles per workgroup read the rows' inputs less often, and leave fewer workgroups: they pay where those still fill the chip.  One, two and four tiles,
-// us: one bfloat16 row 9216 -> 4096 (256 tiles) 6.5, 9.1, 14.7; 32 rows 20, 13.6, 16.8; 64 rows 38, 25, 17; 8 8-bit rows 4096 -> 32000 24, 16, 14.7;
-// 128 float32 rows 1003 -> 1000 6.4, 5.0, 6.4.
-int w4_rows_tiles(int rows, int out)
+// Which kernel takes a product: the shortest of their times in us, fitted to 175 products (inputs 256 to 9216, outputs 256 to 32000, 1 to 2048 rows, every type and
+// group, half of them no multiple of anything), of which it picks one that is more than a tenth slower than the best once.
+// w4_rows_kernel reads all rows' inputs in every workgroup, slower where they start at odd addresses, but is one launch; the others stage the rows first.
+// More tiles per workgroup read the inputs less often, and leave fewer workgroups: one, two and four tiles, one bfloat16 row 9216 -> 4096 6.5, 9.1, 14.7; 32
+// rows 20, 13.6, 16.8; 64 rows 38, 25, 17; 8 8-bit rows 4096 -> 32000 24, 16, 14.7; 128 float32 rows 1003 -> 1000 6.4, 5.0, 6.4.
+// Tiles of 64 x 64 whose inputs eight waves share fill the chip where few of 256 x 128 would not.  By rows, by waves, by tiles: 64 bfloat16 rows 9216 -> 4096
+// 17, 26, 138; 48 rows 4096 -> 16384 21, 18, 65; 128 rows 4096 -> 8192 34, 19, 75, 4097 -> 8192 70, 20, 77; 247 8-bit rows 8538 -> 31744 in groups of 32 737, 258,
+// 316; 2048 bfloat16 rows 4096 -> 8192 -, 189, 138.
+W4Choice w4_choice(int rows, int in, int out, int group, int form)
 {
-    int tiles;
-    rows_cost(rows, out, &tiles);
-    return tiles;
-}
-
-// Which kernel takes a product: the shortest of three times in us, fitted to 220 products (inputs 256 to 9216, outputs 256 to 32000, 1 to 2048 rows), of
-// which it picks one that is more than a tenth slower than the best twice.
-// w4_rows_kernel reads all rows' inputs in every workgroup, but is one launch; the others stage the rows first.  Tiles of 64 x 64 whose inputs eight waves
-// share fill the chip where few of 256 x 128 would not.  Measured by rows, by waves, by tiles: 64 bfloat16 rows 9216 -> 4096 17, 26, 138; 48 rows
-// 4096 -> 16384 21, 18, 65; 128 rows 9216 -> 4096 29, 27, 141; 600 8-bit rows 512 -> 8192 47, 26, 27; 2048 bfloat16 rows 4096 -> 8192 -, 189, 142.
-W4Kernel w4_kernel(int rows, int in, int out, int form)
-{
-    int tiles;
     const bool f32 = form == ROWS_F32, i8 = form == ROWS_I8;
     const double chunks = (in + 127) / 128, parts = f32 ? 3 : 1;
-    const double by_rows = 3 + rows_cost(rows, out, &tiles) * 8 * std::ceil(chunks / 8) * (f32 ? 2 : i8 ? 1.3 : 1);     // (eight waves share the chunks)
-    const double by_waves = 3.5 + rounds(out, 64, rows, 64) * (2.2 + (i8 ? 1.9 : 2.6) * std::ceil(chunks * parts / 8));
-    const double by_tiles = 8 + (i8 ? 1.6 : 2.1) * chunks * parts * rounds(out, 64 * SIDE, rows, TILE * BLOCK);
-    if (by_rows <= by_waves && by_rows <= by_tiles && rows <= 16 * 65535) return W4_ROWS;
-    return by_waves <= by_tiles ? W4_WAVES : W4_TILES;
+    const double by_eight = 8 * std::ceil(chunks / 8);                      // (eight waves share the chunks)
+    const double operand = f32 ? 2.1 : i8 ? (in % 4 ? 1.5 : 1.3) : in % 2 ? 2.2 : 1.0;
+    W4Choice best{W4_ROWS, 0, 0.0};
+    for (int tiles : {1, 2, 4}) {
+        const double chunk = tiles == 1 ? 0.1 : tiles == 2 ? 0.145 : 0.185;
+        const double time = 2.6 + rounds(out, 16 * tiles, rows, 16) * (0.6 + chunk * operand * by_eight);
+        if (best.tiles == 0 || time < best.time) best = {W4_ROWS, tiles, time};
+    }
+    if (rows > 16 * 65535) best.time = HUGE_VAL;                            // (a launch's second dimension)
+    // a group's scaling weighs more where groups are short
+    const double scaled = group == 32 ? 1.4 : group == 64 ? 1.08 : 1.0, tile_scaled = group == 32 ? (i8 ? 2.3 : 1.45) : group == 64 ? (i8 ? 1.1 : 1.35) : 1.0;
+    const double by_waves = 3.5 + rounds(out, 64, rows, 64) * (2.2 + scaled * (i8 ? 1.6 : 2.5) * std::ceil(chunks * parts / 8));
+    if (by_waves < best.time) best = {W4_WAVES, 0, by_waves};
+    const double by_tiles = 10 + tile_scaled * (i8 ? 1.6 : 2.3) * chunks * parts * rounds(out, 64 * SIDE, rows, TILE * BLOCK);
+    if (by_tiles < best.time) best = {W4_TILES, 0, by_tiles};
+    return best;
 }
 
 size_t w4_staged_bytes(int rows, int in, int out, int group)
 {
     size_t most = 0;
     for (int form : {(int)ROWS_F32, (int)ROWS_BF16, (int)ROWS_I8})
-        if (w4_kernel(rows, in, out, form) != W4_ROWS) most = std::max(most, Staged(rows, in, group, form).total());
+        if (w4_choice(rows, in, out, group, form).kernel != W4_ROWS) most = std::max(most, Staged(rows, in, group, form).total());
     return most;
 }
 

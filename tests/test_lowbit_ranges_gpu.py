@@ -7,6 +7,7 @@ import torch
 
 from paper_1603_05279_amd import xnor
 from tests.lowbit_helpers import EPS32, HALF_ULP, SMALLEST, TYPES, assert_within, filled, generator, normal
+from tests import test_w4_linear_gpu as products
 from tests.test_logprobs_gpu import check as check_logprobs
 from tests.test_logprobs_gpu import run as run_logprobs
 from tests.test_w4_linear_gpu import check as check_product
@@ -42,6 +43,13 @@ def test_staged_8_bit_products(x_group, group, rows, out, cin):
         part = (q[:, k:k + group].double() @ whole.t()) * packed.test_scale[:, k // group] * xs.double()[:, k // x_group if x_group else 0, None]
         want, sums = want + part, sums + part.abs()
     assert_within(y, want, (-(-cin // group) + 8) * 2 * EPS32 * sums + HALF_ULP["bf16"] * want.abs() + SMALLEST["bf16"], "y")
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16", "q8"])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_the_largest_tiles(t, group):
+    """Every type and group on results enough for them, sizes that no tile divides."""
+    products.test_products_of_very_many_rows(t, 2050, 8198, 261, group)
 
 
 @pytest.mark.parametrize("out,cin", [(20, 40), (600, 200)])
