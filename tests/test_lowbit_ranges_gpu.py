@@ -29,7 +29,7 @@ def test_staged_products(t, group, rows, out, cin):
 
 @pytest.mark.parametrize("x_group", [0, 128])
 @pytest.mark.parametrize("group", [32, 64, 128])
-@pytest.mark.parametrize("rows,out,cin", STAGED)
+@pytest.mark.parametrize("rows,out,cin", STAGED + [(200, 4000, 1024), (131, 4001, 2048)])
 def test_staged_8_bit_products(x_group, group, rows, out, cin):
     gen = generator(rows + group + x_group)
     packed, w, _ = make(gen, out, cin, group, True)
@@ -83,7 +83,7 @@ def test_infinities_and_nan_in_staged_rows(t, rows, out, cin):
 
 def test_8_bit_rows_whose_scale_is_nan():
     gen = generator(9)
-    for rows, out, cin in ((5, 100, 300), (200, 4000, 1030), (2100, 8200, 520)):
+    for rows, out, cin in ((5, 100, 300), (200, 4000, 1030), (200, 4000, 1024), (2100, 8200, 520)):
         packed, _, _ = make(gen, out, cin, 64, False)
         q = torch.randint(-127, 128, (rows, cin), generator=gen, dtype=torch.int8).cuda()
         for x_group in (0, 64):
