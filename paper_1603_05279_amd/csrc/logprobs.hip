@@ -390,6 +390,7 @@ __global__ __launch_bounds__(THREADS) void logprobs_wave_kernel(LogprobArgs a, i
     };
     // the list's best in order: keys differ, so every rank is taken once
     auto rank_list = [&]() {
+        wave_fence();
         int kept = n > 64 ? 0 : n;
         if (n > 64) raise_bound();                  // (a long list is thinned out first)
         for (int i = 0; i < n && n > 64; i += 64) {
