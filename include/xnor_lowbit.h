@@ -95,7 +95,8 @@ XNOR_API int xnor_w4_pack(const uint8_t *codes, const float *scale, const uint8_
                           void *hip_stream);
 
 /*
- * Products of rows with 4-bit weights:  y[r][o] = sum_k x[r][k] w[o][k], summed in float32 group by group, rounded once.
+ * Products of rows with 4-bit weights:  y[r][o] = sum_k x[r][k] w[o][k], summed in float32, rounded once.  A real row's sums hold 16 + u in place of
+ * u - zero, and what that adds is taken out group by group, or four groups at a time: roundings are relative to sum |x| 32 scale over four groups.
  *   xnor_w4_linear      x `type` [rows][in], apart by x_stride  ->  y `type` [rows][out].  The products are exact (16-bit rows as they
  *       are, float32 rows as three bfloat16 numbers); a row that holds an infinity or a NaN gives NaN
  *   xnor_w4_linear_q8   q int8 [rows][in] with x_scale float32 [rows][ceil(in / x_group)] (one per row where x_group is 0), as

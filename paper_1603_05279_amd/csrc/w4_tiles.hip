@@ -15,8 +15,7 @@ constexpr int TILE = 16, BLOCK = 8;         // rows or outputs of a matrix instr
 // What the rows become (the first kernel writes it, the second reads it), in a workspace of the caller's:
 //   operands  [block of 128 rows][chunk of 128 inputs][part][tile of 16 rows][step][lane][16 bytes]: 16 bits, 4 steps of 32 inputs; 8 bits, 2 steps
 //             of 64.  Tiles past the last row are not written: they meet no result that is kept
-//   sums      [tile of 16 rows][quad of groups][lane][16 bytes], 16 bits only: the groups' sums of x as three bfloat16 numbers in an order that
-//             gives all products with a second factor's three but the smallest: lane 16 i + r is row r, group i of the quad
+//   sums      [tile of 16 rows][quad of groups][lane] float32, 16 bits only: the groups' sums of x, lane 16 i + r is row r, group i of the quad
 //   scales    [tile of 16 rows][group][row] float32, 8-bit rows with scales of groups only
 struct Staged {
     int blocks, chunks, parts, groups, quads;
@@ -26,26 +25,16 @@ struct Staged {
           groups((in + group - 1) / group), quads(form == ROWS_I8 ? 0 : (groups + 3) / 4), bytes(form == ROWS_I8) {}
     __host__ __device__ int tile_bytes() const { return bytes ? 2048 : 4096; }
     __host__ __device__ size_t sums_at() const { return (size_t)blocks * chunks * parts * BLOCK * tile_bytes(); }
-    __host__ __device__ size_t scales_at() const { return sums_at() + (size_t)blocks * BLOCK * quads * 1024; }
+    __host__ __device__ size_t scales_at() const { return sums_at() + (size_t)blocks * BLOCK * quads * 256; }
     __host__ __device__ size_t total() const { return scales_at() + (bytes ? (size_t)blocks * BLOCK * groups * 64 : 0); }
 };
 
-// x cut off to three bfloat16 numbers whose sum it is (an infinity has no rest)
-__device__ __forceinline__ void three_parts(float x, uint32_t *p)
+// What four groups' offset and zero points add to the totals of 16 outputs x 16 rows, taken out: - scale (OFFSET + zero) of a lane's output and group (its
+// quarter) times the group's sum of a lane's row, four groups in one instruction.  It multiplies and adds in 32 bits: bfloat16 parts of both factors in the
+// instructions of the products leave a part of every sum out that has a sign (2.9e-6 of the results' size where this leaves 5e-7).
+template <int X> __device__ __forceinline__ f32x4 less_offset(f32x4 total, float scale, uint8_t zero, float sum)
 {
-    const bool finite = __builtin_fabsf(x) < __builtin_inff();
-    p[0] = (__float_as_uint(x) | (x != x ? 0x00400000u : 0u)) >> 16;
-    const float rest = finite ? x - __uint_as_float(p[0] << 16) : 0.0f;
-    p[1] = __float_as_uint(rest) >> 16;
-    p[2] = __float_as_uint(rest - __uint_as_float(p[1] << 16)) >> 16;
-}
-
-// - scale (OFFSET + zero) as three bfloat16 numbers in the order that meets those of a group's sum
-template <int X> __device__ __forceinline__ bf16x8 offset_parts(float scale, uint8_t zero)
-{
-    uint32_t p[3];
-    three_parts(-(scale * (Form<X>::OFFSET + (float)zero)), p);
-    return __builtin_bit_cast(bf16x8, u32x4{p[0] | p[0] << 16, p[1] | p[1] << 16, p[0] | p[2] << 16, p[1] | p[2] << 16});
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(-(scale * (Form<X>::OFFSET + (float)zero)), sum, total, 0, 0, 0);
 }
 
 struct StageArgs {
@@ -113,13 +102,11 @@ __global__ __launch_bounds__(256) void w4_stage_kernel(StageArgs a)
             sum[1] = sum[2] + sum[3];
         }
         if (steps == 4) sum[0] += sum[1];
-        u32x4 *sums = reinterpret_cast<u32x4 *>(a.staged + st.sums_at()) + (size_t)tile * st.quads * 64;
+        float *sums = reinterpret_cast<float *>(a.staged + st.sums_at()) + (size_t)tile * st.quads * 64;
         const int last = chunk == st.chunks - 1 ? 4 * st.quads : first + per_chunk;
         for (int g = first + quarter; g < last; g += 4) {
             const int i = g - first;
-            uint32_t p[3];
-            three_parts(i >= per_chunk ? 0.0f : i == 0 ? sum[0] : i == 1 ? sum[1] : i == 2 ? sum[2] : sum[3], p);
-            sums[(size_t)(g >> 2) * 64 + (g & 3) * 16 + r] = u32x4{p[0] | p[1] << 16, p[0] | p[1] << 16, p[2] | p[0] << 16, p[2] | p[1] << 16};
+            sums[(size_t)g * 16 + r] = i >= per_chunk ? 0.0f : i == 0 ? sum[0] : i == 1 ? sum[1] : i == 2 ? sum[2] : sum[3];
         }
     }
 }
@@ -131,6 +118,14 @@ struct TileArgs {
     int rows, in, out, type, form;
     int row_blocks, out_blocks;
 };
+
+// The lane's number, made anew: what a loop without a register to spare does not keep (a spilled one would come back behind all loads on their way).
+__device__ __forceinline__ int lane_anew()
+{
+    uint32_t none = 0;
+    asm volatile("" : "+s"(none));
+    return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, none));
+}
 
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
 typedef const __attribute__((address_space(1))) uint8_t global_u8;
@@ -161,6 +156,9 @@ __global__ __launch_bounds__(128 * SIDE) void w4_tiles_kernel(TileArgs a)
     typedef Form<X> F;
     typedef TilePlace<X, STEPS, GROUPED, SIDE> P;
     constexpr int WAVES = P::WAVES, AHEAD = BUFFERS - 1, TB = P::TB, PER_CHUNK = P::PER_CHUNK;
+    // 16 bits: groups of 32 leave no register for a lane's places; groups of 128 leave enough for what is taken out to be loaded ahead of a step's products
+    // (behind them 144 us in place of 140)
+    constexpr bool SPARE = X == ROWS_I8 || STEPS > 1, EARLY = STEPS == 4;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const W4Layout l(a.out, a.in, 32 * STEPS);
     const Staged st(a.rows, a.in, 32 * STEPS, a.form);
@@ -204,8 +202,14 @@ __global__ __launch_bounds__(128 * SIDE) void w4_tiles_kernel(TileArgs a)
         for (int i = 0; i < BLOCK * TB / (WAVES * 1024); ++i) to_lds(from + i * WAVES * 1024 + at, to + (i * WAVES + wave) * 1024);
 #pragma unroll
         for (int i = 0; i < 2; ++i) to_lds(codes_from[i] + (size_t)c * 1024 + lane_at, to + P::CODES + (wave * 2 + i) * 1024);
-        if (lane < SCALE_LANES)
-            to_lds(scales_from + (scale_off + (uint32_t)min(g0 + f / 4 % PER_CHUNK, l.groups - 1) * 64), to + P::SCALES + wo * P::FACTORS + wr * SCALE_LANES * 16);
+        if constexpr (SPARE) {
+            if (lane < SCALE_LANES)
+                to_lds(scales_from + (scale_off + (uint32_t)min(g0 + f / 4 % PER_CHUNK, l.groups - 1) * 64), to + P::SCALES + wo * P::FACTORS + wr * SCALE_LANES * 16);
+        } else if (const int now = lane_anew(); now < SCALE_LANES) {
+            const int f = now + wr * SCALE_LANES;
+            to_lds(scales_from + ((uint32_t)min(f / (4 * PER_CHUNK), more) * l.groups + min(g0 + f / 4 % PER_CHUNK, l.groups - 1)) * 64 + (f & 3) * 16,
+                   to + P::SCALES + wo * P::FACTORS + wr * SCALE_LANES * 16);
+        }
         if (GROUPED && lane < ROW_LANES)
             to_lds(row_scales_from + (row_off + (uint32_t)min(g0 + fr / 4 % PER_CHUNK, l.groups - 1) * 64),
                    to + P::ROW_SCALES + wr * P::FACTORS + wo * ROW_LANES * 16);
@@ -219,24 +223,34 @@ __global__ __launch_bounds__(128 * SIDE) void w4_tiles_kernel(TileArgs a)
         for (int j = 0; j < 4; ++j) total[i][j] = f32x4{0, 0, 0, 0};
 #pragma unroll
     for (int r = 0; r < AHEAD; ++r) fetch(min(r, steps - 1), r);
-    // what the offset and the zero points add is taken out first, while the first chunks arrive: - scale (OFFSET + zero) times the groups' sums, four
-    // groups per instruction, both factors as three bfloat16 numbers (all products but the smallest: 2^-32 of the largest)
-    if constexpr (X != ROWS_I8) {
-        const u32x4 *sums = reinterpret_cast<const u32x4 *>(a.staged + st.sums_at()) + (size_t)rtile * st.quads * 64 + lane;
-        for (int quad = 0; quad < st.quads; ++quad) {
-            bf16x8 b[4];
+    // What the offset and the zero points add is taken out beside the sums that hold it, in the middle of every four groups, so that the total is never
+    // further from the result than their terms.  2048 float32 rows of one sign, 9216 -> 4096: off by 5.6e-7 of the results' size in groups of 128, 7.9e-7 of
+    // 32 (a 32-bit library product of the real weights 3.9e-7; all groups taken out at once 1.1e-5 and 6.4e-5).
+    const int per_quad = STEPS * parts;          // steps of four groups
+    int quad = 0, due = X == ROWS_I8 ? -1 : min((per_quad - 1) / 2, steps - 1);
+    float sum_out[4], scale_out[4];
+    uint32_t zeros_out[4];
+    auto load_out = [&]() {
+        const int now = SPARE ? lane : lane_anew();
+        const float *sums = reinterpret_cast<const float *>(a.staged + st.sums_at()) + ((size_t)rtile * st.quads + quad) * 64;
+        const uint32_t at = min(4 * quad + (now >> 4), l.groups - 1) * 16 + (now & 15);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) b[j] = __builtin_bit_cast(bf16x8, sums[((size_t)j * st.quads + quad) * 64]);
-            const int g = min(4 * quad + quarter, l.groups - 1);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const size_t f = ((size_t)min(otile + i, l.tiles - 1) * l.groups + g) * 16 + col;
-                const bf16x8 k = offset_parts<X>(reinterpret_cast<const float *>(scales)[f], zeros[f]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) total[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, b[j], total[i][j], 0, 0, 0);
-            }
+        for (int i = 0; i < 4; ++i) {
+            const size_t tile = (size_t)min(otile + i, l.tiles - 1) * l.groups * 16;
+            sum_out[i] = (sums + (size_t)i * st.quads * 64)[now];
+            scale_out[i] = (reinterpret_cast<const float *>(scales) + tile)[at];
+            zeros_out[i] = (zeros + tile)[at];
         }
-    }
+    };
+    auto take_out = [&]() {
+        if constexpr (X != ROWS_I8)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) total[i][j] = less_offset<X>(total[i][j], scale_out[i], (uint8_t)zeros_out[i], sum_out[j]);
+        ++quad;
+        due = quad < st.quads ? min(due + per_quad, steps - 1) : -1;
+    };
     // A group's sums wait in acc, with the factors they are scaled by, until the first product of the next group takes their place: the scaling
     // fills the time that the next chunk's operands take from LDS, and that a product takes.
     constexpr int WIDE = X == ROWS_I8 && STEPS >= 2 ? 2 : 1, PHASES = 4 / WIDE;        // steps of 32 inputs per product, products per chunk
@@ -266,6 +280,7 @@ __global__ __launch_bounds__(128 * SIDE) void w4_tiles_kernel(TileArgs a)
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"((AHEAD - 1) * P::LOADS) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
+        if (X != ROWS_I8 && EARLY && s == due) load_out();
         const uint8_t *here = lds + place * P::BYTES, *x = here + wr * 4 * TB + lane_at, *wc = here + P::CODES + wo * 4096 + lane_at;
         const uint8_t *sw = here + P::SCALES + wo * P::FACTORS + quarter * 16, *sx = here + P::ROW_SCALES + wr * P::FACTORS + col * 4;
         const uint8_t *zero = here + P::ZEROS + wo * P::FACTORS / 4 + col;
@@ -322,6 +337,10 @@ __global__ __launch_bounds__(128 * SIDE) void w4_tiles_kernel(TileArgs a)
                     for (int j = 0; j < 4; ++j) row_factor[j] = *reinterpret_cast<const float *>(sx + (j * PER_CHUNK + g) * 64);
             }
         }
+        if (X != ROWS_I8 && s == due) {
+            if (!EARLY) load_out();
+            take_out();
+        }
         __builtin_amdgcn_s_waitcnt(0xc07f);                           // lgkmcnt(0): its reads of the place are over at the next barrier
         asm volatile("" ::: "memory");
     }
@@ -369,6 +388,7 @@ __global__ __launch_bounds__(512) void w4_waves_kernel(TileArgs a)
         zeros[i] = a.image + l.zero_at() + tile * l.groups * 16 + col;
     }
     const float *row_scales = reinterpret_cast<const float *>(a.staged + st.scales_at()) + (size_t)rtile * l.groups * 16 + col;
+    const float *sums = reinterpret_cast<const float *>(a.staged + st.sums_at()) + (size_t)rtile * st.quads * 64;
     const u32x4 *rows_from = reinterpret_cast<const u32x4 *>(a.staged + ((size_t)(rtile / BLOCK) * st.chunks * st.parts * BLOCK + rtile % BLOCK) * TB) + lane;
     f32x4 total[4][4];
 #pragma unroll
@@ -384,6 +404,20 @@ __global__ __launch_bounds__(512) void w4_waves_kernel(TileArgs a)
         f32x4 f[PER_CHUNK][4];
         float c[PER_CHUNK][4];
         uint32_t z[PER_CHUNK][4];
+        // What the offset and the zero points add to the wave's next STEPS chunks, four groups, is taken out before their sums (as in w4_tiles_kernel; 256
+        // float32 rows of one sign, 9216 -> 4096: off by 3e-7 to 6.5e-7).  The lane's group of them:
+        const int own = min((chunk + quarter / PER_CHUNK * WAVES) * PER_CHUNK + quarter % PER_CHUNK, l.groups) * 16 + col;
+        const bool real = own < l.groups * 16;
+        const int own_at = real ? own : col;
+        float sum[4], scale[4];
+        uint8_t zero_point[4];
+        if (X != ROWS_I8)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                sum[i] = sums[(size_t)i * st.quads * 64 + own_at];
+                scale[i] = scales[i][own_at];
+                zero_point[i] = zeros[i][own_at - col];
+            }
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = codes[i][(size_t)chunk * 64];
 #pragma unroll
@@ -401,6 +435,12 @@ __global__ __launch_bounds__(512) void w4_waves_kernel(TileArgs a)
             }
         }
         __builtin_amdgcn_sched_barrier(0);
+        if constexpr (X != ROWS_I8)
+            if (s == chunk * st.parts && chunk / WAVES % STEPS == 0)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) total[i][j] = less_offset<X>(total[i][j], real ? scale[i] : 0.0f, zero_point[i], sum[j]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             typename F::acc_t acc[4];
@@ -434,21 +474,6 @@ __global__ __launch_bounds__(512) void w4_waves_kernel(TileArgs a)
                         if (GROUPED) part *= c[t / STEPS][j];
                         total[i][j][v] = __builtin_fmaf(f[t / STEPS][i][v], part, total[i][j][v]);
                     }
-            }
-        }
-    }
-    if constexpr (X != ROWS_I8) {                   // the offset and the zero points, as in w4_tiles_kernel
-        const u32x4 *sums = reinterpret_cast<const u32x4 *>(a.staged + st.sums_at()) + (size_t)rtile * st.quads * 64 + lane;
-        for (int quad = wave; quad < st.quads; quad += WAVES) {
-            bf16x8 b[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) b[j] = __builtin_bit_cast(bf16x8, sums[((size_t)j * st.quads + quad) * 64]);
-            const int g = min(4 * quad + quarter, l.groups - 1);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const bf16x8 k = offset_parts<X>(scales[i][(size_t)g * 16 + col], zeros[i][(size_t)g * 16]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) total[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, b[j], total[i][j], 0, 0, 0);
             }
         }
     }
