@@ -14,23 +14,24 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 // pair form: the top of the mantissa under a fixed exponent.  What that and the zero point add to a sum is the same multiple of the group's sum
 // of x for all inputs and is taken out with it:
 //     sum x (u - z) = sum x (16 + u) - (16 + z) sum x
+// bfloat16 takes a 4096th of that, and the results are multiplied by it at the end: the sums of 128 inputs of float32's whole range stay within it.
 // For 8-bit rows it enters as u - z, seven instructions for eight codes, and the sums are exact.  Float32 rows are three bfloat16 numbers each
 // whose sum they are.
 enum { ROWS_F32 = XNOR_F32, ROWS_BF16 = XNOR_BF16, ROWS_F16 = XNOR_F16, ROWS_I8 = 3 };
 
 template <int X> struct Form {          // 16 bits
     static constexpr int PARTS = X == ROWS_F32 ? 3 : 1;
-    static constexpr float OFFSET = 16.0f;
+    static constexpr float OFFSET = 16.0f, BACK = X == ROWS_F16 ? 1.0f : 4096.0f;        // BACK: what a result is multiplied by
     typedef f32x4 acc_t;
     typedef u32x4 operand_t;
-    static __device__ __forceinline__ operand_t ones()
+    static __device__ __forceinline__ operand_t ones()          // 1 / BACK
     {
-        const uint32_t one = X == ROWS_F16 ? 0x3c003c00u : 0x3f803f80u;
+        const uint32_t one = X == ROWS_F16 ? 0x3c003c00u : 0x39803980u;
         return operand_t{one, one, one, one};
     }
     static __device__ __forceinline__ operand_t widen(uint32_t w)
     {
-        uint32_t mask = X == ROWS_F16 ? 0x03c003c0u : 0x00780078u, base = X == ROWS_F16 ? 0x4c004c00u : 0x41804180u;
+        uint32_t mask = X == ROWS_F16 ? 0x03c003c0u : 0x00780078u, base = X == ROWS_F16 ? 0x4c004c00u : 0x3b803b80u;
         asm("" : "+v"(mask), "+v"(base));           // (in registers: an and-or takes no two literals)
         if (X == ROWS_F16) return operand_t{(w << 6 & mask) | base, (w << 2 & mask) | base, (w >> 2 & mask) | base, (w >> 6 & mask) | base};
         return operand_t{(w << 3 & mask) | base, (w >> 1 & mask) | base, (w >> 5 & mask) | base, (w >> 9 & mask) | base};

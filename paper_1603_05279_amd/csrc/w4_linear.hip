@@ -228,7 +228,8 @@ __global__ __launch_bounds__(64 * WAVES) void w4_rows_kernel(W4Args a)
     f32x4 s = *reinterpret_cast<const f32x4 *>(&red[0][r][4 * q]);
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) s += *reinterpret_cast<const f32x4 *>(&red[w][r][4 * q]);
-    if (X == ROWS_I8 && !GROUPED) s *= a.x_scale[row];
+    if constexpr (X != ROWS_I8) s *= F::BACK;
+    else if (!GROUPED) s *= a.x_scale[row];
     store_four(a.y, a.type, (size_t)row * a.out + o, s, a.out - o);
 }
 

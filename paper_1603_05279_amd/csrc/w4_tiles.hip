@@ -15,7 +15,7 @@ constexpr int TILE = 16, BLOCK = 8;         // rows or outputs of a matrix instr
 // What the rows become (the first kernel writes it, the second reads it), in a workspace of the caller's:
 //   operands  [block of 128 rows][chunk of 128 inputs][part][tile of 16 rows][step][lane][16 bytes]: 16 bits, 4 steps of 32 inputs; 8 bits, 2 steps
 //             of 64.  Tiles past the last row are not written: they meet no result that is kept
-//   sums      [tile of 16 rows][quad of groups][lane] float32, 16 bits only: the groups' sums of x, lane 16 i + r is row r, group i of the quad
+//   sums      [tile of 16 rows][quad of groups][lane] float32, 16 bits only: the groups' sums of SHARE x, lane 16 i + r is row r, group i of the quad
 //   scales    [tile of 16 rows][group][row] float32, 8-bit rows with scales of groups only
 struct Staged {
     int blocks, chunks, parts, groups, quads;
@@ -29,12 +29,16 @@ struct Staged {
     __host__ __device__ size_t total() const { return scales_at() + (bytes ? (size_t)blocks * BLOCK * groups * 64 : 0); }
 };
 
+// The factors of what is taken out, BACK between them: a group's sum and 32 scales stay within float32's range.
+template <int X> constexpr float SHARE = Form<X>::BACK == 1.0f ? 1.0f : 1.0f / 128.0f;
+
 // What four groups' offset and zero points add to the totals of 16 outputs x 16 rows, taken out: - scale (OFFSET + zero) of a lane's output and group (its
 // quarter) times the group's sum of a lane's row, four groups in one instruction.  It multiplies and adds in 32 bits: bfloat16 parts of both factors in the
 // instructions of the products leave a part of every sum out that has a sign (2.9e-6 of the results' size where this leaves 5e-7).
 template <int X> __device__ __forceinline__ f32x4 less_offset(f32x4 total, float scale, uint8_t zero, float sum)
 {
-    return __builtin_amdgcn_mfma_f32_16x16x4f32(-(scale * (Form<X>::OFFSET + (float)zero)), sum, total, 0, 0, 0);
+    constexpr float rest = 1.0f / (Form<X>::BACK * SHARE<X>);
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(-(scale * __builtin_fmaf((float)zero, rest, Form<X>::OFFSET * rest)), sum, total, 0, 0, 0);
 }
 
 struct StageArgs {
@@ -91,7 +95,7 @@ __global__ __launch_bounds__(256) void w4_stage_kernel(StageArgs a)
             for (int p = 0; p < F::PARTS; ++p) out[(size_t)p * BLOCK * 256 + j * 64] = b[p];
             float s = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s += v[j].v[i];
+            for (int i = 0; i < 8; ++i) s = __builtin_fmaf(v[j].v[i], SHARE<X>, s);
             s += __shfl_xor(s, 16, 64);
             s += __shfl_xor(s, 32, 64);
             sum[j] = s;
@@ -355,7 +359,8 @@ __global__ __launch_bounds__(128 * SIDE) void w4_tiles_kernel(TileArgs a)
         for (int i = 0; i < 4; ++i) {
             const int o = (otile + i) * TILE + 4 * quarter;
             f32x4 v = total[i][j];
-            if (X == ROWS_I8 && !GROUPED) v *= c;
+            if constexpr (X != ROWS_I8) v *= F::BACK;
+            else if (!GROUPED) v *= c;
             store_four(a.y, a.type, (size_t)row * a.out + o, v, a.out - o);
         }
     }
@@ -489,7 +494,8 @@ __global__ __launch_bounds__(512) void w4_waves_kernel(TileArgs a)
         f32x4 v = *reinterpret_cast<const f32x4 *>(red + r * PITCH + q);
 #pragma unroll
         for (int k = 1; k < WAVES; ++k) v += *reinterpret_cast<const f32x4 *>(red + (k * 64 + r) * PITCH + q);
-        if (X == ROWS_I8 && !GROUPED) v *= a.x_scale[row];
+        if constexpr (X != ROWS_I8) v *= F::BACK;
+        else if (!GROUPED) v *= a.x_scale[row];
         store_four(a.y, a.type, (size_t)row * a.out + o, v, a.out - o);
     }
 }

@@ -9,7 +9,7 @@ import pytest
 import torch
 
 from paper_1603_05279_amd import xnor
-from tests.lowbit_helpers import EPS32, apart, assert_within, filled, generator, normal
+from tests.lowbit_helpers import EPS32, HALF_ULP, TYPES, apart, assert_within, filled, generator, normal
 from tests.test_w4_linear_gpu import codes_of, scratch
 
 pytestmark = pytest.mark.gpu
@@ -73,3 +73,26 @@ def test_single_terms_keep_their_24_bits(rows, out, cin, group):
     at, value = at[some], x.amax(1)[some].double()[:, None]
     s, z = scale[:, at // group].t().double(), zero[:, at // group].t().double()
     assert_within(y[some.cuda()], value * s * (u[:, at].t().double() - z), 8 * EPS32 * 31 * value * s, "single terms")
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("rows,out,cin", [(5, 100, 300), (20, 1000, 1003), (200, 4000, 1030), (2100, 8200, 520)])
+def test_rows_as_large_as_their_type(rows, out, cin, group, t):
+    """Finite rows of any size give finite results: sums of 16 + u terms must not leave the range that those of u - z keep."""
+    gen = generator(rows + group)
+    u, scale, zero, _ = weights(gen, out, cin, group)
+    scale = scale * 1e-3
+    packed = xnor.W4Weights(codes_of(u).cuda(), scale.cuda(), zero.cuda(), cin, group)
+    largest = torch.finfo(TYPES[t]).max
+    x = (torch.rand((rows, cin), generator=gen) * 2 - 1) * largest
+    x[0], x[1], x[2] = largest, -largest, torch.where(torch.arange(cin) % 2 == 0, largest, -largest)
+    x = x.to(TYPES[t])
+    y = filled((rows, out), TYPES[t])
+    xnor.xnor_w4_linear(x.cuda(), packed.wimg, y, scratch(rows, cin, out, group), rows, cin, out, group)
+    some = torch.cat((torch.arange(5), torch.randint(0, rows, (50,), generator=gen)))
+    whole = u.double() - zero.double().repeat_interleave(group, 1)[:, :cin]
+    want = x[some].double() @ (whole * scale.double().repeat_interleave(group, 1)[:, :cin]).t()
+    # (every rounding relative to 62 scales of the row's sum, 4 of them for each 32 inputs, added at random: eight standard deviations)
+    bound = 8 * math.sqrt(4 * cin / 32) * EPS32 * 62 * x[some].double().abs().amax(1)[:, None] * 512 * scale.double().amax(1)
+    assert_within(y[some.cuda()], want, bound + HALF_ULP[t] * want.abs(), "y")
