@@ -38,8 +38,9 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const void *w, long lo
                 lo = fminf(lo, __shfl_xor(lo, s, 64));
                 hi = fmaxf(hi, __shfl_xor(hi, s, 64));
             }
-            const float span = zero ? hi - lo : fmaxf(hi, -lo), levels = zero ? 15.0f : 7.0f;
-            const bool some = span >= TINY;
+            // (halves of both: the span of float32's largest of either sign is not a float32 number)
+            const float span = zero ? 0.5f * hi - 0.5f * lo : 0.5f * fmaxf(hi, -lo), levels = zero ? 7.5f : 3.5f;
+            const bool some = span >= 0.5f * TINY;
             const float inverse = some ? levels / span : 0.0f;
             const float z = zero ? __builtin_rintf(-lo * inverse) : 8.0f;
             uint32_t word = 0;

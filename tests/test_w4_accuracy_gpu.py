@@ -96,3 +96,24 @@ def test_rows_as_large_as_their_type(rows, out, cin, group, t):
     # (every rounding relative to 62 scales of the row's sum, 4 of them for each 32 inputs, added at random: eight standard deviations)
     bound = 8 * math.sqrt(4 * cin / 32) * EPS32 * 62 * x[some].double().abs().amax(1)[:, None] * 512 * scale.double().amax(1)
     assert_within(y[some.cuda()], want, bound + HALF_ULP[t] * want.abs(), "y")
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_weights_as_large_as_their_type(t, zeros):
+    """Finite weights have finite scales, and codes within half a step of them (and a zero point's half, with zero points)."""
+    gen = generator(17)
+    out, cin, group = 9, 300, 32
+    largest = torch.finfo(TYPES[t]).max
+    w = ((torch.rand((out, cin), generator=gen) * 2 - 1) * largest).to(TYPES[t])
+    w[0, :2], w[1], w[2] = torch.tensor([largest, -largest]), largest, -largest
+    groups = -(-cin // group)
+    codes, scale = filled((out, 16 * -(-cin // 32)), torch.uint8), filled((out, groups), torch.float32)
+    zero = filled((out, groups), torch.uint8) if zeros else None
+    xnor.xnor_w4_quantize(w.cuda(), codes, scale, zero, out, cin, group)
+    codes = codes.cpu()
+    u = torch.stack((codes & 15, codes >> 4), -1).flatten(1)[:, :cin].double()
+    z = (zero.cpu() if zeros else torch.full((out, groups), 8)).double().repeat_interleave(group, 1)[:, :cin]
+    s = scale.cpu().double().repeat_interleave(group, 1)[:, :cin]
+    assert scale.isfinite().all() and (scale > 0).all()
+    assert (((u - z) * s - w.double()).abs() <= (1.001 if zeros else 0.501) * s).all()
