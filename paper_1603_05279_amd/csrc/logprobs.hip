@@ -197,14 +197,16 @@ __device__ __forceinline__ void finish_row(const LogprobArgs &a, size_t row, Sta
 {
     const int i = threadIdx.x % WIDTH;
     const bool empty = st.m == -__builtin_inff() && !(st.s != st.s);
-    const float log_s = empty ? 0.0f : __builtin_logf(st.s), base = empty ? 0.0f : st.m;
+    // (the sum holds the largest logit's own term, 1: below it is a rounding, which would make its log probability positive.  Likewise the entropy.  A NaN stays)
+    const float log_s = empty || st.s < 1.0f ? 0.0f : __builtin_logf(st.s), base = empty ? 0.0f : st.m;
     if (i == 0) {
         if (a.lse) a.lse[row] = empty ? -__builtin_inff() : base + log_s;
         if (a.shift) {
             a.shift[2 * row] = st.m;
             a.shift[2 * row + 1] = log_s;
         }
-        if (a.entropy) a.entropy[row] = empty ? 0.0f : log_s - st.t / st.s;
+        const float entropy = log_s - st.t / st.s;
+        if (a.entropy) a.entropy[row] = empty || entropy < 0.0f ? 0.0f : entropy;
     }
     for (int g = i; g < a.given; g += WIDTH) {
         if (g >= WIDTH) own = given_at<TYPE>(a, row, g);
