@@ -15,6 +15,7 @@
  *  - rows = 0 is a call without work: XNOR_OK, nothing is launched and no pointer is looked at.
  *  - Where two kernels are enqueued, the first may be when the second reports XNOR_ERR_HIP; it writes that call's own outputs or
  *    workspace only.  A workspace's contents are undefined afterwards, and nothing in it has to be cleared before.
+ *  - What a ..._workspace_bytes call says never falls as rows grows: a workspace for more rows serves fewer rows of the same other sizes.
  */
 #ifndef XNOR_LOWBIT_H
 #define XNOR_LOWBIT_H

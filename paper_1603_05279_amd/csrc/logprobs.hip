@@ -576,20 +576,24 @@ __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(LogprobGradArgs 
 
 // Parts of a row: few rows are spread over the chip, workgroups (no alternatives) or waves.  Fewer waves leave SIMDs idle, more repeat each part's search and
 // are joined in a second launch: 1500 bfloat16 rows of 32000, 20 alternatives, 40 us in two parts, 47 in one; 512 rows 22 in eight, 25 in four, 30 in two.
+int logprobs_spread(int top) { return top ? 4096 : 512; }
 int logprobs_parts(int rows, int vocab, int top)
 {
     const int longest = (vocab + 2047) / 2048;
     if (vocab <= (top ? 64 * 8 * STEPS : CHUNK)) return 1;
-    return std::max(1, std::min({longest, (top ? 4096 : 512) / std::max(rows, 1), MOST_PARTS}));
+    return std::max(1, std::min({longest, logprobs_spread(top) / std::max(rows, 1), MOST_PARTS}));
 }
 int logprobs_per_part(int vocab, int parts) { return ((vocab + parts - 1) / parts + 7) / 8 * 8; }
 
 }  // namespace
 
+bool logprobs_needs(int rows, int vocab, int top) { return logprobs_parts(rows, vocab, top) > 1; }
+
 size_t logprobs_workspace_bytes(int rows, int vocab, int top)
 {
-    const int parts = logprobs_parts(rows, vocab, top);
-    return parts == 1 ? 0 : (size_t)rows * parts * (16 + 8 * (size_t)top);
+    // the parts of up to `rows` rows: as many as a row has at most, and no more together than are spread over the chip
+    const int each = logprobs_parts(1, vocab, top);
+    return each == 1 ? 0 : (size_t)std::min((long long)rows * each, (long long)logprobs_spread(top)) * (16 + 8 * (size_t)top);
 }
 
 xnor_status launch_logprobs(const void *logits, long long stride, const void *tokens, int token_bytes, float *logprob, float *lse, float *shift, float *entropy,

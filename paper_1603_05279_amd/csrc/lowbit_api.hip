@@ -45,7 +45,7 @@ int xnor_rmsnorm_q8(const void *x, int64_t x_stride, const void *residual, int64
 size_t xnor_rmsnorm_backward_workspace_bytes(int rows, int cols)
 {
     if (rows <= 0 || rows > MAX_ROWS || cols <= 0 || cols > MAX_COLS) return 0;
-    return (size_t)rmsnorm_grad_parts(rows, cols) * (size_t)cols * sizeof(float);
+    return rmsnorm_grad_workspace_bytes(rows, cols);
 }
 
 int xnor_rmsnorm_backward(const void *h, int64_t h_stride, const float *rstd, const float *weight, const void *g_values, int64_t g_stride,
@@ -95,7 +95,7 @@ int xnor_w4_linear(const void *x, int64_t x_stride, const void *wimg, void *y, v
     if (xnor_status s = check_w4(out, in, group)) return s;
     if (!known_type(type)) return XNOR_ERR_UNSUPPORTED;
     if (rows == 0) return XNOR_OK;
-    if (!x || !wimg || !y || (!workspace && w4_linear_workspace_bytes(rows, in, out, group))) return XNOR_ERR_NULL;
+    if (!x || !wimg || !y || (!workspace && w4_linear_needs(rows, in, out, group, type))) return XNOR_ERR_NULL;
     if (x_stride < in) return XNOR_ERR_SHAPE;
     if (!aligned16(x, wimg, y, workspace)) return XNOR_ERR_ALIGN;
     return launch_w4_linear(x, x_stride, wimg, y, workspace, rows, in, out, group, type, (hipStream_t)hip_stream);
@@ -108,7 +108,7 @@ int xnor_w4_linear_q8(const int8_t *q, const float *x_scale, const void *wimg, v
     if (xnor_status s = check_w4(out, in, group)) return s;
     if (!known_type(type) || (x_group != 0 && (!w4_group(x_group) || x_group < group))) return XNOR_ERR_UNSUPPORTED;
     if (rows == 0) return XNOR_OK;
-    if (!q || !x_scale || !wimg || !y || (!workspace && w4_linear_workspace_bytes(rows, in, out, group))) return XNOR_ERR_NULL;
+    if (!q || !x_scale || !wimg || !y || (!workspace && w4_linear_needs(rows, in, out, group, W4_8_BITS))) return XNOR_ERR_NULL;
     if (!aligned16(q, x_scale, wimg, y, workspace)) return XNOR_ERR_ALIGN;
     return launch_w4_linear_q8(q, x_scale, wimg, y, workspace, rows, in, out, group, x_group, type, (hipStream_t)hip_stream);
 }
@@ -124,7 +124,7 @@ int xnor_logprobs(const void *logits, int64_t stride, const void *tokens, int to
     if (xnor_status s = check_logprobs(token_bytes, rows, vocab, given, top, type)) return s;
     if (rows == 0) return XNOR_OK;
     if (!logits || (given && (!tokens || !logprob)) || (top && (!top_index || !top_logprob)) ||
-        (!workspace && logprobs_workspace_bytes(rows, vocab, top)))
+        (!workspace && logprobs_needs(rows, vocab, top)))
         return XNOR_ERR_NULL;
     if (stride < vocab) return XNOR_ERR_SHAPE;
     if (!aligned16(logits, tokens, logprob, lse, shift, entropy, top_index, top_logprob, workspace)) return XNOR_ERR_ALIGN;

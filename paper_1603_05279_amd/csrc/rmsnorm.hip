@@ -305,14 +305,20 @@ template <class F> void by_steps(int steps, F f)
 struct GradShape {
     int beside, parts;
 };
+static int grad_most(int cols) { return row_shape(cols).threads > 512 ? 256 : 512; }
 static GradShape grad_shape(int rows, int cols)
 {
     if (rows == 0) return {1, 0};
-    const int waves = row_shape(cols).threads / 64, beside = std::max(1, 8 / waves), most = waves > 8 ? 256 : 512;
+    const int waves = row_shape(cols).threads / 64, beside = std::max(1, 8 / waves), most = grad_most(cols);
     const int sets = (rows + beside - 1) / beside, turns = (sets + most - 1) / most;
     return {beside, (sets + turns - 1) / turns};
 }
-int rmsnorm_grad_parts(int rows, int cols) { return grad_shape(rows, cols).parts; }
+// Enough for up to `rows` rows: an even share of the turns takes fewer workgroups, never more.
+size_t rmsnorm_grad_workspace_bytes(int rows, int cols)
+{
+    const GradShape s = grad_shape(rows, cols);
+    return (size_t)std::min((rows + s.beside - 1) / s.beside, grad_most(cols)) * cols * sizeof(float);
+}
 
 xnor_status launch_rmsnorm_q8(const void *x, long long x_stride, const void *residual, long long residual_stride, const float *weight,
                               void *sum_out, int8_t *q, float *scale, void *values, float *rstd, int rows, int cols, int group, int type,

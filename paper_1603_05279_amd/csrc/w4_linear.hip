@@ -280,8 +280,6 @@ xnor_status launch_w4_pack(const uint8_t *codes, const float *scale, const uint8
     return hip_status(hipGetLastError());
 }
 
-size_t w4_linear_workspace_bytes(int rows, int in, int out, int group) { return w4_staged_bytes(rows, in, out, group); }
-
 xnor_status launch_w4_linear(const void *x, long long x_stride, const void *wimg, void *y, void *workspace, int rows, int in, int out, int group, int type,
                              hipStream_t stream)
 {

@@ -10,6 +10,8 @@ namespace xnor {
 
 namespace {
 
+static_assert(ROWS_I8 == W4_8_BITS);
+
 constexpr int TILE = 16, BLOCK = 8;         // rows or outputs of a matrix instruction, such tiles of a workgroup's side
 
 // What the rows become (the first kernel writes it, the second reads it), in a workspace of the caller's:
@@ -549,11 +551,10 @@ static double rounds(int out, int outs, int rows, int height)
 // Tiles of 64 x 64 whose inputs eight waves share fill the chip where few of 256 x 128 would not.  By rows, by waves, by tiles: 64 bfloat16 rows 9216 -> 4096
 // 17, 26, 138; 48 rows 4096 -> 16384 21, 18, 65; 128 rows 4096 -> 8192 34, 19, 75, 4097 -> 8192 70, 20, 77; 247 8-bit rows 8538 -> 31744 in groups of 32 737, 258,
 // 316; 2048 bfloat16 rows 4096 -> 8192 -, 189, 138.
-W4Choice w4_choice(int rows, int in, int out, int group, int form)
+static W4Choice by_rows(int rows, int in, int out, int form)
 {
     const bool f32 = form == ROWS_F32, i8 = form == ROWS_I8;
-    const double chunks = (in + 127) / 128, parts = f32 ? 3 : 1;
-    const double by_eight = 8 * std::ceil(chunks / 8);                      // (eight waves share the chunks)
+    const double by_eight = 8 * std::ceil((in + 127) / 128 / 8.0);          // (eight waves share the chunks)
     const double operand = f32 ? 2.1 : i8 ? (in % 4 ? 1.5 : 1.3) : in % 2 ? 2.2 : 1.0;
     W4Choice best{W4_ROWS, 0, 0.0};
     for (int tiles : {1, 2, 4}) {
@@ -562,20 +563,33 @@ W4Choice w4_choice(int rows, int in, int out, int group, int form)
         if (best.tiles == 0 || time < best.time) best = {W4_ROWS, tiles, time};
     }
     if (rows > 16 * 65535) best.time = HUGE_VAL;                            // (a launch's second dimension)
-    // a group's scaling weighs more where groups are short
-    const double scaled = group == 32 ? 1.4 : group == 64 ? 1.08 : 1.0, tile_scaled = group == 32 ? (i8 ? 2.3 : 1.45) : group == 64 ? (i8 ? 1.1 : 1.35) : 1.0;
-    const double by_waves = 3.5 + rounds(out, 64, rows, 64) * (2.2 + scaled * (i8 ? 1.6 : 2.5) * std::ceil(chunks * parts / 8));
-    if (by_waves < best.time) best = {W4_WAVES, 0, by_waves};
-    const double by_tiles = 10 + tile_scaled * (i8 ? 1.6 : 2.3) * chunks * parts * rounds(out, 64 * SIDE, rows, TILE * BLOCK);
-    if (by_tiles < best.time) best = {W4_TILES, 0, by_tiles};
     return best;
 }
+static W4Choice staged(int rows, int in, int out, int group, int form)
+{
+    const bool i8 = form == ROWS_I8;
+    const double steps = (in + 127) / 128 * (form == ROWS_F32 ? 3.0 : 1.0);
+    // a group's scaling weighs more where groups are short
+    const double scaled = group == 32 ? 1.4 : group == 64 ? 1.08 : 1.0, tile_scaled = group == 32 ? (i8 ? 2.3 : 1.45) : group == 64 ? (i8 ? 1.1 : 1.35) : 1.0;
+    const double by_waves = 3.5 + rounds(out, 64, rows, 64) * (2.2 + scaled * (i8 ? 1.6 : 2.5) * std::ceil(steps / 8));
+    const double by_tiles = 10 + tile_scaled * (i8 ? 1.6 : 2.3) * steps * rounds(out, 64 * SIDE, rows, TILE * BLOCK);
+    return by_tiles < by_waves ? W4Choice{W4_TILES, 0, by_tiles} : W4Choice{W4_WAVES, 0, by_waves};
+}
+W4Choice w4_choice(int rows, int in, int out, int group, int form)
+{
+    const W4Choice one = by_rows(rows, in, out, form), two = staged(rows, in, out, group, form);
+    return two.time < one.time ? two : one;
+}
 
-size_t w4_staged_bytes(int rows, int in, int out, int group)
+bool w4_linear_needs(int rows, int in, int out, int group, int form) { return w4_choice(rows, in, out, group, form).kernel != W4_ROWS; }
+
+// Enough for up to `rows` rows of any type.  Neither time falls as rows grows, so rows are staged nowhere up to where w4_rows_kernel takes no longer than the
+// others for one row.
+size_t w4_linear_workspace_bytes(int rows, int in, int out, int group)
 {
     size_t most = 0;
     for (int form : {(int)ROWS_F32, (int)ROWS_BF16, (int)ROWS_I8})
-        if (w4_choice(rows, in, out, group, form).kernel != W4_ROWS) most = std::max(most, Staged(rows, in, group, form).total());
+        if (by_rows(rows, in, out, form).time > staged(1, in, out, group, form).time) most = std::max(most, Staged(rows, in, group, form).total());
     return most;
 }
 
