@@ -407,13 +407,25 @@ class PackedWeights:
         xnor_pack_weights(w, self.wbits, self.alpha, self.wmfma, k_out, c, kh, kw, stream)
 
 
+def on_stream(stream):
+    """torch's work and memory on the stream that a call is given (None: as it is)."""
+    if stream is None or isinstance(stream, torch.cuda.Stream):
+        return torch.cuda.stream(stream)
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream.cuda_stream))
+
+
 class W4Weights:
-    """The image of 4-bit weights that the products read (`wimg`), packed from codes, scale and zero (None: 8 everywhere)."""
+    """The image of 4-bit weights that the products read (`wimg`), packed from codes, scale and zero (None: 8 everywhere).
+
+    With a `stream` the memory is taken there, where it is written, and kept for the current stream too."""
 
     def __init__(self, codes, scale, zero, in_features, group, stream=None):
         out_features = codes.shape[0]
         self.shape, self.group = (out_features, in_features), group
-        self.wimg = torch.empty((w4_wimg_bytes(out_features, in_features, group),), dtype=torch.uint8, device=codes.device)
+        with on_stream(stream):
+            self.wimg = torch.empty((w4_wimg_bytes(out_features, in_features, group),), dtype=torch.uint8, device=codes.device)
+        if stream is not None:
+            self.wimg.record_stream(torch.cuda.current_stream(codes.device))
         xnor_w4_pack(codes, scale, zero, self.wimg, out_features, in_features, group, stream)
 
     @classmethod
@@ -421,9 +433,10 @@ class W4Weights:
         """From real weights [out][in], rounded by xnor_w4_quantize (zeros: with zero points)."""
         out_features, in_features = w.shape
         groups = -(-in_features // group)
-        codes = torch.empty((out_features, 16 * -(-in_features // 32)), dtype=torch.uint8, device=w.device)
-        scale = torch.empty((out_features, groups), dtype=torch.float32, device=w.device)
-        zero = torch.empty((out_features, groups), dtype=torch.uint8, device=w.device) if zeros else None
+        with on_stream(stream):                 # (given back while the calls may be waiting there: to that stream, behind them)
+            codes = torch.empty((out_features, 16 * -(-in_features // 32)), dtype=torch.uint8, device=w.device)
+            scale = torch.empty((out_features, groups), dtype=torch.float32, device=w.device)
+            zero = torch.empty((out_features, groups), dtype=torch.uint8, device=w.device) if zeros else None
         xnor_w4_quantize(w, codes, scale, zero, out_features, in_features, group, stream)
         return cls(codes, scale, zero, in_features, group, stream)
 
