@@ -60,20 +60,25 @@ class EndTraining:
         self.logprob, self.shift = empty(rows, 1), empty(rows, 2)
         self.g_logprob = torch.full((rows, 1), -1.0 / rows, device=device)
         self.g_x, self.g_norm_weight, self.g_logits = empty(rows, width), empty(width), empty(rows, classes)
+        self.g_weight = empty(classes, width)
         nbytes = max(xnor.rmsnorm_backward_workspace_bytes(rows, width), xnor.logprobs_workspace_bytes(rows, classes, 0))
         self.workspace = empty(max(nbytes, 1), dtype=torch.uint8)
 
     def gradients(self, x, labels, stream=None):
-        """Loss = -mean logprob; fills g_x, g_norm_weight and g_weight."""
+        """Loss = -mean logprob; fills g_x, g_norm_weight and g_weight, all on `stream`."""
+        with xnor.on_stream(stream):
+            self._gradients(x, labels)
+
+    def _gradients(self, x, labels):
         classes, width = self.weight.shape
         rows = self.rows
-        xnor.xnor_rmsnorm_q8(x, None, self.norm_weight, None, None, None, self.values, self.rstd, rows, width, self.group, EPS, stream)
+        xnor.xnor_rmsnorm_q8(x, None, self.norm_weight, None, None, None, self.values, self.rstd, rows, width, self.group, EPS)
         logits = self.values @ self.weight.t()
-        xnor.xnor_logprobs(logits, labels, self.logprob, None, self.shift, None, None, None, self.workspace, rows, classes, 1, 0, stream)
-        xnor.xnor_logprobs_backward(logits, labels, self.shift, None, self.g_logprob, None, self.g_logits, rows, classes, 1, stream)
-        self.g_weight = self.g_logits.t() @ self.values
+        xnor.xnor_logprobs(logits, labels, self.logprob, None, self.shift, None, None, None, self.workspace, rows, classes, 1, 0)
+        xnor.xnor_logprobs_backward(logits, labels, self.shift, None, self.g_logprob, None, self.g_logits, rows, classes, 1)
+        torch.mm(self.g_logits.t(), self.values, out=self.g_weight)
         xnor.xnor_rmsnorm_backward(x, self.rstd, self.norm_weight, self.g_logits @ self.weight, None, self.g_x, self.g_norm_weight,
-                                   self.workspace, rows, width, stream)
+                                   self.workspace, rows, width)
 
     def step(self, x, labels, rate):
         self.gradients(x, labels)
