@@ -104,7 +104,7 @@ def run(rows=1024, inputs=1024, width=512, classes=1000, steps=90, group=64, rat
     layer = xnor.PackedWeights(torch.randn((width, inputs, 1, 1), generator=gen).cuda())
     labels = torch.randint(0, classes, (2, rows), generator=gen)
     x = patterns[labels] + torch.randn((2, rows, inputs), generator=gen)
-    labels = labels.cuda().unsqueeze(2)
+    labels = [part.cuda().unsqueeze(1) for part in labels]              # (apart: each starts at 16 bytes, whatever the rows)
     train, held = (binary_features(part.cuda(), layer) for part in x)
 
     end = EndTraining(torch.ones(width, device="cuda"), torch.zeros((classes, width), device="cuda"), rows, group)
