@@ -253,7 +253,8 @@ template <int TYPE, int HELD, bool ENTROPY> __device__ __forceinline__ void take
 }
 
 // Wide rows whose alternatives nobody asks for.  A workgroup takes one part of a row (per_part logits; parts = 1: the row) chunk by chunk, the next chunk's
-// loads ahead of the sums; each thread keeps statistics of its own logits.  What bounds it: the memory (4096 x 32000 bfloat16 with entropy 51 us, 5.1 TB/s),
+// loads ahead of the sums; each thread keeps statistics of its own logits.  What bounds it: the memory (4096 x 32000 bfloat16 with entropy 52 us, 5.0 TB/s; 71 right behind a
+// backward pass, whose last writes are on their way),
 // for few rows two launches and their trips to memory (1 x 128000 6.7 us).
 template <int TYPE, bool ENTROPY>
 __global__ __launch_bounds__(THREADS) void logprobs_kernel(LogprobArgs a)
@@ -522,7 +523,8 @@ struct LogprobGradArgs {
 
 // One pass: g = -p (G + g_entropy (log p + entropy)) with G = sum g_logprob, and the tokens' own terms added before the store.
 // A row, or a part of it, belongs to the WIDTH threads of a workgroup or of a wave.  What bounds it: the memory (4096 x 32000 bfloat16 97 us, read and write
-// 5.4 TB/s; 300 x 50257 float32 20 us, 5.9).
+// 5.4 TB/s, 84 right behind the forward pass; 300 x 50257 float32 20 us, 5.9).  Every thread looks at every given token, so many of them cost: 4 108 us, 16 194,
+// 64 566, 1024 8.4 ms.
 template <int TYPE, int STEPS, int WIDTH>
 __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(LogprobGradArgs a, int rows)
 {

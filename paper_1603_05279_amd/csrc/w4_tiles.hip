@@ -144,10 +144,11 @@ __device__ __forceinline__ void to_lds(const uint8_t *from, uint8_t *to)        
 // STEPS of 32 inputs per group.  2 * SIDE waves, each 64 outputs x 64 rows, together 64 * SIDE outputs x 128 rows.  All a chunk needs (the rows' operands,
 // codes, scales, zero points) goes straight to one of BUFFERS places in LDS, BUFFERS - 1 chunks ahead, one barrier per chunk.  Every wave issues
 // the same number of loads for a chunk, so that it can wait for its oldest chunk alone.  GROUPED: 8-bit rows with scales of groups.
-// What bounds it: the matrix instructions at the clock that the chip holds under them.  2048 bfloat16 rows 4096 -> 8192, groups of 128: 138 us with the staging,
-// 1.0 PFLOP/s (a library's product with bfloat16 weights 99); the same loop of matrix instructions alone takes 92, 16 cycles each at 1.43 GHz, the loads into
-// LDS add 15, the scaling 9, reading LDS 5, widening the codes nothing; launches, staging, first loads and stores are 18.  Groups of 32 198 us, 8 bits 121.
-// Instructions of 32 x 32 results: 156, 248, 122; the next chunk's first operands read ahead of the barrier: 149.
+// What bounds it: matrix and vector instructions, of which the waves leave a chunk's barrier with the same ones to do, so that they hardly overlap.  2048 bfloat16
+// rows 4096 -> 8192, groups of 128: 141 us with the staging, 0.98 PFLOP/s (a library's product with bfloat16 weights 99); of the cycles, at 2.2 GHz, the matrix
+// pipes are busy in 0.44 and vector instructions take 0.35.  Groups of 64 199 us, of 32 219 (four times the scaling; what is taken out is half as much matrix
+// work again).  8 bits 120, 208, 316: 0.23 and 0.61 in groups of 128 (converting, scaling twice, widening).  Float32 rows, three products: 360, 497, 505.
+// Tried when groups of 128 took 138: instructions of 32 x 32 results 156, the next chunk's first operands read ahead of the barrier 149.
 template <int X, int STEPS, bool GROUPED, int SIDE> struct TilePlace {
     static constexpr int WAVES = 2 * SIDE, PER_CHUNK = 4 / STEPS, TB = X == ROWS_I8 ? 2048 : 4096;
     static constexpr int ROWS = 0, CODES = BLOCK * TB, SCALES = CODES + SIDE * 4096, FACTORS = 4 * PER_CHUNK * 64;      // of four tiles
@@ -371,8 +372,8 @@ __global__ __launch_bounds__(128 * SIDE) void w4_tiles_kernel(TileArgs a)
 
 // The same sums where there are too few tiles of that size: a workgroup makes 64 outputs x 64 rows, its eight waves take every eighth chunk (its parts
 // one after another), operands straight to registers, and add their sums in LDS.
-// What bounds it: the caches (256 bfloat16 rows 9216 -> 4096: each workgroup reads 1.5 MB, 61 bytes per ns and CU, 15.6 TB/s together; 32 us with the staging,
-// 8 bits 26).  The same loads a chunk ahead, through LDS, 34 and 27.
+// What bounds it: the caches, and vector instructions between a step's loads (256 bfloat16 rows 9216 -> 4096: each workgroup reads 1.5 MB, some 60 bytes per ns and
+// CU; 30 us with the staging.  8 bits 25, vector instructions half of the cycles).  The same loads a chunk ahead, through LDS, were 1 to 2 us slower.
 template <int X, int STEPS, bool GROUPED>
 __global__ __launch_bounds__(512) void w4_waves_kernel(TileArgs a)
 {
@@ -550,7 +551,7 @@ static double rounds(int out, int outs, int rows, int height)
 // rows 20, 13.6, 16.8; 64 rows 38, 25, 17; 8 8-bit rows 4096 -> 32000 24, 16, 14.7; 128 float32 rows 1003 -> 1000 6.4, 5.0, 6.4.
 // Tiles of 64 x 64 whose inputs eight waves share fill the chip where few of 256 x 128 would not.  By rows, by waves, by tiles: 64 bfloat16 rows 9216 -> 4096
 // 17, 26, 138; 48 rows 4096 -> 16384 21, 18, 65; 128 rows 4096 -> 8192 34, 19, 75, 4097 -> 8192 70, 20, 77; 247 8-bit rows 8538 -> 31744 in groups of 32 737, 258,
-// 316; 2048 bfloat16 rows 4096 -> 8192 -, 189, 138.
+// 316; 2048 bfloat16 rows 4096 -> 8192 -, 189, 141.
 static W4Choice by_rows(int rows, int in, int out, int form)
 {
     const bool f32 = form == ROWS_F32, i8 = form == ROWS_I8;
