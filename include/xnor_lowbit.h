@@ -139,7 +139,8 @@ XNOR_API int xnor_logprobs(const void *logits, int64_t stride, const void *token
 /*
  * Backward pass of logprob and entropy:
  *     g_logits_j = sum_i g_logprob[i] ([token[i] = j] - p_j) - g_entropy p_j (log p_j + entropy)
- * A masked logit (-inf) has gradient 0, and so has all of a row without any other; what is no token takes no part.
+ * A masked logit (-inf) has gradient 0, and so has all of a row without any other; what is no token takes no part.  A p below 2^-126 counts
+ * as 0.
  *   logits, tokens             in   as above
  *   shift, entropy             in   of the forward pass; entropy may be NULL without g_entropy
  *   g_logprob                  in   (nullable) float32 [rows][given]
