@@ -100,7 +100,7 @@ XNOR_API int xnor_w4_pack(const uint8_t *codes, const float *scale, const uint8_
  * u - zero, and what that adds is taken out group by group, or four groups at a time: roundings are relative to sum |x| 32 scale over four groups.
  *   xnor_w4_linear      x `type` [rows][in], apart by x_stride  ->  y `type` [rows][out].  The products are exact (16-bit rows as they
  *       are, float32 rows as three bfloat16 numbers); a row that holds an infinity or a NaN gives NaN.  Finite rows of
- *       any size do not, where sum |x| scale over four groups is below 2^134; an infinity is then a result beyond the type's range
+ *       any size do not, where sum |x| scale over four groups is below 2^134 (float16: 2^122); an infinity is then a result beyond the type's range
  *   xnor_w4_linear_q8   q int8 [rows][in] with x_scale float32 [rows][ceil(in / x_group)] (one per row where x_group is 0), as
  *       xnor_rmsnorm_q8 writes them: x = q * x_scale  ->  y `type` [rows][out].  The sums of a group are exact integers.
  *       x_group is 0, 32, 64 or 128, and not below group otherwise (XNOR_ERR_UNSUPPORTED)
