@@ -3,7 +3,8 @@
  *
  * XNOR-Net leaves a network's first and last layers real (sec. 4.1).  These calls run what stands there: the residual's addition
  * and the root-mean-square norm with 8-bit outputs, products with 4-bit weights under group scales, and the log probabilities of
- * the answer.  The conventions are those of xnor.h (device pointers that the caller owns, 16-byte aligned; enqueued on hip_stream
+ * the answer; in 8 bits the products, activation functions that keep their input for the backward pass, the gradients of weights, and
+ * tokens drawn from the answer.  The conventions are those of xnor.h (device pointers that the caller owns, 16-byte aligned; enqueued on hip_stream
  * without synchronising; nothing is allocated or kept; an xnor_status comes back, arguments are checked before anything is
  * launched), with these additions:
  *  - Real tensors hold one xnor_dtype; sums, norms and statistics are held in float32 whatever it is, and a result is rounded
@@ -150,6 +151,104 @@ XNOR_API int xnor_logprobs(const void *logits, int64_t stride, const void *token
 XNOR_API int xnor_logprobs_backward(const void *logits, int64_t stride, const void *tokens, int token_bytes, const float *shift,
                                     const float *entropy, const float *g_logprob, const float *g_entropy, void *g_logits, int rows,
                                     int vocab, int given, int type, void *hip_stream);
+
+/*
+ * Rows to 8 bits:  per row and group of neighbouring columns  top = max |x|,  q = round(x * (127 / top)), halves to even,  scale = top / 127
+ *   x      in   `type` [rows][cols], apart by x_stride; cols up to 2^24
+ *   q      out  int8 [rows][cols]
+ *   scale  out  float32 [rows][groups], groups = ceil(cols / group) (1 where group is 0: one scale for the whole row)
+ *   group       0, 32, 64 or 128 columns; the last group of a row may be shorter
+ * A group whose top is below 2^-100 is q = 0 with scale 0; one that holds an infinity or a NaN is q = 0 with scale NaN.
+ * Rows of weights [out][in] with group 0 give what xnor_w8_linear takes as w and w_scale.
+ */
+XNOR_API int xnor_q8_rows(const void *x, int64_t x_stride, int8_t *q, float *scale, int rows, int cols, int group, int type, void *hip_stream);
+
+/*
+ * Products of 8-bit rows with 8-bit weights, a scale for each row and output:
+ *     y[r][o] = (sum_k q[r][k] w[o][k]) * (x_scale[r] * w_scale[o]) + bias[o]
+ * The sums are exact integers; a result is finite where it is within float32's range, whatever the scales, and one product of the scales is rounded to
+ * float32 before the sum is multiplied by it.
+ *   q        in   int8 [rows][in] with x_scale float32 [rows]: as xnor_q8_rows, xnor_rmsnorm_q8 and xnor_activation_q8 write them with group 0
+ *   w        in   int8 [out][in] with w_scale float32 [out]
+ *   bias     in   (nullable) float32 [out]
+ *   y        out  `type` [rows][out]
+ *   workspace     xnor_w8_linear_workspace_bytes(rows, in, out) bytes, may be NULL where that is 0
+ * in <= 131071 (sums within 32 bits), XNOR_ERR_UNSUPPORTED otherwise.
+ */
+XNOR_API size_t xnor_w8_linear_workspace_bytes(int rows, int in, int out);
+XNOR_API int xnor_w8_linear(const int8_t *q, const float *x_scale, const int8_t *w, const float *w_scale, const float *bias, void *y, void *workspace,
+                            int rows, int in, int out, int type, void *hip_stream);
+
+/*
+ * Activation functions, whose input is kept in 8 bits for the backward pass and whose values may go to the next product in 8 bits:
+ *     a = f(x)                                    gated 0: x [rows][cols]
+ *     a = f(x[:, :cols]) * x[:, cols:]            gated 1: x [rows][2 cols]
+ *     f: XNOR_RELU max(x, 0);  XNOR_GELU x Phi(x), Phi the normal distribution;  XNOR_SILU x / (1 + exp(-x));  in float32
+ *   x           in   `type` [rows][cols or 2 cols], apart by x_stride
+ *   y           out  (nullable) `type` [rows][cols]: a
+ *   q, scale    out  (nullable) int8 [rows][cols], float32 [rows][ceil(cols / group) or 1]: what xnor_q8_rows makes of a in float32
+ *   kept, kept_scale
+ *               out  (nullable) int8 [rows][cols or 2 cols], float32 [rows][groups of kept_group of those columns, or 1]: what xnor_q8_rows makes of x
+ *   group, kept_group   0, 32, 64 or 128 columns
+ * One of y, q and kept is required.  cols <= 2^23.
+ *
+ * Backward pass, from what was kept: with x^ = kept * kept_scale
+ *     g_x = g_y f'(x^),  f'(0) = 0 for XNOR_RELU;     gated: g_x[:, :cols] = g_y x^[:, cols:] f'(x^[:, :cols]),  g_x[:, cols:] = g_y f(x^[:, :cols])
+ *   g_y         in   `type` [rows][cols], apart by g_stride
+ *   g_x         out  `type` [rows][cols or 2 cols]; may be g_y itself where that is dense and gated is 0
+ */
+typedef enum {
+    XNOR_RELU = 0,
+    XNOR_GELU = 1,
+    XNOR_SILU = 2
+} xnor_function;
+
+XNOR_API int xnor_activation_q8(const void *x, int64_t x_stride, void *y, int8_t *q, float *scale, int8_t *kept, float *kept_scale, int rows, int cols,
+                                int group, int kept_group, int function, int gated, int type, void *hip_stream);
+XNOR_API int xnor_activation_backward(const int8_t *kept, const float *kept_scale, const void *g_y, int64_t g_stride, void *g_x, int rows, int cols,
+                                      int kept_group, int function, int gated, int type, void *hip_stream);
+
+/*
+ * Gradients of a product's weights and bias from the 8-bit rows that it read:
+ *     g_w[o][k] = sum_r g_y[r][o] q[r][k] scale[r][k / group],     g_bias[o] = sum_r g_y[r][o]
+ *   q, scale    in   int8 [rows][in], float32 [rows][ceil(in / group)] (one per row where group is 0)
+ *   g_y         in   `type` [rows][out], apart by g_stride
+ *   g_w         out  `w_type` [out][in]; accumulate 1: added to what it holds, in float32, and rounded once more
+ *   g_bias      out  (nullable) float32 [out]; accumulate as above
+ *   workspace        xnor_q8_weight_gradient_workspace_bytes(rows, in, out, group, type, w_type) bytes
+ * The products run on the 16-bit matrix instructions with float32 sums.  A row's value q * scale enters as one 11-bit float where w_type is XNOR_BF16, as two (22 bits)
+ * otherwise; a float32 gradient likewise; 16-bit gradients enter as they are.  Both sides are first multiplied by powers of two that bring each column's largest to 2^15,
+ * and what is 2^-29 of that or less keeps its value to 2^-40 of it.  A row of g_w whose gradients hold an infinity or a NaN is not finite; neither are a group's columns
+ * with a scale that is not.  The order of the sums follows from the sizes alone.
+ * With rows = 0 the results are zeros (accumulate: left as they are).
+ */
+XNOR_API size_t xnor_q8_weight_gradient_workspace_bytes(int rows, int in, int out, int group, int type, int w_type);
+XNOR_API int xnor_q8_weight_gradient(const int8_t *q, const float *scale, const void *g_y, int64_t g_stride, void *g_w, float *g_bias, int accumulate,
+                                     void *workspace, int rows, int in, int out, int group, int type, int w_type, void *hip_stream);
+
+/*
+ * Draws a token for each row of logits, with random numbers that are given.  The tokens of a row are ordered by their logits, the largest first, of equal ones the
+ * lowest index first, and have weights exp((l - largest) / temperature).  Drawn from are
+ *     the first top_k;  of these the shortest run from the first on whose weights reach top_p of theirs;  of these the ones whose weight is min_p or more
+ * and drawn is the first of them whose weights, added up in that order, exceed uniform times their sum.
+ *   logits       in   `type` [rows][vocab], apart by stride; -inf marks what is masked, and is never drawn
+ *   temperature  in   (nullable: 1) float32 [rows], >= 0; 0 draws the first token
+ *   top_k        in   (nullable) int32 [rows]; 0 and below: all
+ *   top_p        in   (nullable) float32 [rows]; 1 and above: all; always one token at least
+ *   min_p        in   (nullable) float32 [rows]; 0 and below: all; above 1 as 1
+ *   uniform      in   float32 [rows], within [0, 1): below counts as 0, above as the largest number below 1
+ *   token        out  int32 [rows]
+ *   logprob      out  (nullable) float32 [rows]: log of the token's weight over the sum that it was drawn from
+ *   kept         out  (nullable) int32 [rows]: how many tokens it was drawn from
+ *   workspace         xnor_sample_workspace_bytes(rows, vocab) bytes, may be NULL where that is 0
+ * Weights are held as multiples of 2^-44 (of 2^(b - 62) for a vocabulary of 2^b > 2^18) and added as integers, so that a draw depends on no order of additions and
+ * differs from the formula's for a uniform within about 1e-12 of a border only.  Tokens whose weight rounds to 0 are counted, never drawn.
+ * A row without any logit above -inf has token -1, logprob -inf and kept 0; one that holds a NaN or +inf, or whose temperature (NaN or below 0),
+ * top_p, min_p or uniform is none (NaN), token -1, logprob NaN and kept 0.
+ */
+XNOR_API size_t xnor_sample_workspace_bytes(int rows, int vocab);
+XNOR_API int xnor_sample(const void *logits, int64_t stride, const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                         const float *uniform, int32_t *token, float *logprob, int32_t *kept, void *workspace, int rows, int vocab, int type, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -6,6 +6,7 @@
 // Checks of a tensor argument: NULL or a dense device tensor of the stated type, as the callers of xnor.py have always
 // been told; sizes are the caller's, as in the C ABI.  The library's entry points are looked up in the file that xnor.py
 // names (bind), so that another build of it can be called.
+#include <c10/core/impl/DeviceGuardImplInterface.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <dlfcn.h>
@@ -122,10 +123,26 @@ int64_t groups(int64_t cols, int64_t group) { return group > 0 ? (cols + group -
 // Sizes that the library states, for the checks of images and workspaces.
 #define XNOR_QUERIES(X)                                                                               \
     X(xnor_rmsnorm_backward_workspace_bytes) X(xnor_w4_wimg_bytes) X(xnor_w4_linear_workspace_bytes) \
-    X(xnor_logprobs_workspace_bytes)
+    X(xnor_logprobs_workspace_bytes) X(xnor_w8_linear_workspace_bytes)                               \
+    X(xnor_q8_weight_gradient_workspace_bytes) X(xnor_sample_workspace_bytes)
 #define XNOR_QUERY_POINTER(NAME) decltype(&::NAME) p_##NAME = nullptr;
 XNOR_QUERIES(XNOR_QUERY_POINTER)
 void *bytes(PyObject *o, size_t count) { return dense(o, c10::ScalarType::Byte, (int64_t)count); }
+
+// The tensors among a call's arguments (the stream, last, is None or not) have to be on one device, the current one where no stream is given: a kernel would
+// read another's memory, or run on a device that does not hold its tensors.  Returns `value`, so that a call's last number can stand for the check.
+int on_one_device(PyObject *const *a, int n, int value)
+{
+    int device = a[n - 1] == Py_None ? (int)c10::impl::getDeviceGuardImpl(c10::DeviceType::CUDA)->getDevice().index() : -1;
+    for (int i = 0; i < n - 1; ++i) {
+        if (!THPVariable_Check(a[i])) continue;
+        const int here = (int)THPVariable_Unpack(a[i]).get_device();
+        if (device >= 0 && here != device) fail(PyExc_ValueError, "the tensors of a call have to be on the device that it runs on");
+        device = here;
+    }
+    return value;
+}
+int64_t wide(PyObject *cols, PyObject *gated) { return (int64_t)num(cols) << (num(gated) & 1); }
 
 // A descriptor (xnor.py's ctypes structure, nothing else that holds as many bytes) through the buffer protocol; held for the
 // duration of the call.
@@ -237,7 +254,40 @@ void *stream(PyObject *o)
     X(xnor_logprobs_backward, 11, rows(a[0], dtype(a[0]), num(a[7]), num(a[8])), stride(a[0], num(a[7]), num(a[8])),      \
       tokens(a[1], area(a[7], a[9])), token_bytes(a[1]), dense_f32(a[2], 2 * (int64_t)num(a[7])),                         \
       dense_f32(a[3], num(a[7])), dense_f32(a[4], area(a[7], a[9])), dense_f32(a[5], num(a[7])),                          \
-      dense(a[6], scalar_type(dtype(a[0])), area(a[7], a[8])), num(a[7]), num(a[8]), num(a[9]), dtype(a[0]))
+      dense(a[6], scalar_type(dtype(a[0])), area(a[7], a[8])), num(a[7]), num(a[8]), num(a[9]), dtype(a[0]))              \
+    X(xnor_q8_rows, 7, rows(a[0], dtype(a[0]), num(a[3]), num(a[4])), stride(a[0], num(a[3]), num(a[4])),                 \
+      dense_of<int8_t>(a[1], c10::ScalarType::Char, area(a[3], a[4])),                                                    \
+      dense_f32(a[2], num(a[3]) * groups(num(a[4]), num(a[5]))), num(a[3]), num(a[4]), num(a[5]),                         \
+      on_one_device(a, 7, dtype(a[0])))                                                                                   \
+    X(xnor_w8_linear, 11, dense_of<int8_t>(a[0], c10::ScalarType::Char, area(a[7], a[8])), dense_f32(a[1], num(a[7])),    \
+      dense_of<int8_t>(a[2], c10::ScalarType::Char, area(a[9], a[8])), dense_f32(a[3], num(a[9])),                        \
+      dense_f32(a[4], num(a[9])), dense(a[5], scalar_type(dtype(a[5])), area(a[7], a[9])),                                \
+      bytes(a[6], p_xnor_w8_linear_workspace_bytes(num(a[7]), num(a[8]), num(a[9]))), num(a[7]), num(a[8]), num(a[9]),    \
+      on_one_device(a, 11, dtype(a[5])))                                                                                  \
+    X(xnor_activation_q8, 13, rows(a[0], dtype(a[0]), num(a[6]), wide(a[7], a[11])),                                      \
+      stride(a[0], num(a[6]), wide(a[7], a[11])), dense(a[1], scalar_type(dtype(a[0])), area(a[6], a[7])),                \
+      dense_of<int8_t>(a[2], c10::ScalarType::Char, area(a[6], a[7])),                                                    \
+      dense_f32(a[3], num(a[6]) * groups(num(a[7]), num(a[8]))),                                                          \
+      dense_of<int8_t>(a[4], c10::ScalarType::Char, num(a[6]) * wide(a[7], a[11])),                                       \
+      dense_f32(a[5], num(a[6]) * groups(wide(a[7], a[11]), num(a[9]))), num(a[6]), num(a[7]), num(a[8]), num(a[9]),      \
+      num(a[10]), num(a[11]), on_one_device(a, 13, dtype(a[0])))                                                          \
+    X(xnor_activation_backward, 10, dense_of<int8_t>(a[0], c10::ScalarType::Char, num(a[4]) * wide(a[5], a[8])),          \
+      dense_f32(a[1], num(a[4]) * groups(wide(a[5], a[8]), num(a[6]))), rows(a[2], dtype(a[2]), num(a[4]), num(a[5])),    \
+      stride(a[2], num(a[4]), num(a[5])), dense(a[3], scalar_type(dtype(a[2])), num(a[4]) * wide(a[5], a[8])), num(a[4]), \
+      num(a[5]), num(a[6]), num(a[7]), num(a[8]), on_one_device(a, 10, dtype(a[2])))                                      \
+    X(xnor_q8_weight_gradient, 12, dense_of<int8_t>(a[0], c10::ScalarType::Char, area(a[7], a[8])),                       \
+      dense_f32(a[1], num(a[7]) * groups(num(a[8]), num(a[10]))), rows(a[2], dtype(a[2]), num(a[7]), num(a[9])),          \
+      stride(a[2], num(a[7]), num(a[9])), dense(a[3], scalar_type(dtype(a[3])), area(a[9], a[8])),                        \
+      dense_f32(a[4], num(a[9])), num(a[5]),                                                                              \
+      bytes(a[6], p_xnor_q8_weight_gradient_workspace_bytes(num(a[7]), num(a[8]), num(a[9]), num(a[10]), dtype(a[2]),     \
+                                                            dtype(a[3]))),                                                \
+      num(a[7]), num(a[8]), num(a[9]), num(a[10]), dtype(a[2]), on_one_device(a, 12, dtype(a[3])))                        \
+    X(xnor_sample, 13, rows(a[0], dtype(a[0]), num(a[10]), num(a[11])), stride(a[0], num(a[10]), num(a[11])),             \
+      dense_f32(a[1], num(a[10])), dense_of<int32_t>(a[2], c10::ScalarType::Int, num(a[10])), dense_f32(a[3], num(a[10])),\
+      dense_f32(a[4], num(a[10])), dense_f32(a[5], num(a[10])), dense_of<int32_t>(a[6], c10::ScalarType::Int, num(a[10])),\
+      dense_f32(a[7], num(a[10])), dense_of<int32_t>(a[8], c10::ScalarType::Int, num(a[10])),                             \
+      bytes(a[9], p_xnor_sample_workspace_bytes(num(a[10]), num(a[11]))), num(a[10]), num(a[11]),                         \
+      on_one_device(a, 13, dtype(a[0])))
 
 #define XNOR_POINTER(NAME, N, ...) decltype(&::NAME) p_##NAME = nullptr;
 XNOR_CALLS(XNOR_POINTER)

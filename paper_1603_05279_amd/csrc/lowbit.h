@@ -1,4 +1,4 @@
-// Launchers of the calls of xnor_lowbit.h (arguments checked by lowbit_api.hip; rows = 0 reaches none but rmsnorm's backward pass).
+// Launchers of the calls of xnor_lowbit.h (arguments checked by lowbit_api.hip; rows = 0 reaches none but rmsnorm's backward pass and the weights' gradient).
 #pragma once
 #include <hip/hip_runtime.h>
 #include "xnor_lowbit.h"
@@ -42,5 +42,22 @@ xnor_status launch_logprobs(const void *logits, long long stride, const void *to
 xnor_status launch_logprobs_backward(const void *logits, long long stride, const void *tokens, int token_bytes, const float *shift,
                                      const float *entropy, const float *g_logprob, const float *g_entropy, void *g_logits, int rows, int vocab,
                                      int given, int type, hipStream_t stream);
+xnor_status launch_q8_rows(const void *x, long long x_stride, int8_t *q, float *scale, int rows, int cols, int group, int type, hipStream_t stream);
+xnor_status launch_activation_q8(const void *x, long long x_stride, void *y, int8_t *q, float *scale, int8_t *kept, float *kept_scale, int rows, int cols,
+                                 int group, int kept_group, int function, int gated, int type, hipStream_t stream);
+xnor_status launch_activation_backward(const int8_t *kept, const float *kept_scale, const void *g_y, long long g_stride, void *g_x, int rows, int cols,
+                                       int kept_group, int function, int gated, int type, hipStream_t stream);
+size_t w8_linear_workspace_bytes(int rows, int in, int out);
+bool w8_linear_needs(int rows, int in, int out);
+xnor_status launch_w8_linear(const int8_t *q, const float *x_scale, const int8_t *w, const float *w_scale, const float *bias, void *y, void *workspace, int rows,
+                             int in, int out, int type, hipStream_t stream);
+size_t weight_gradient_workspace_bytes(int rows, int in, int out, int group, int type, int w_type);
+xnor_status launch_weight_gradient(const int8_t *q, const float *scale, const void *g_y, long long g_stride, void *g_w, float *g_bias, int accumulate,
+                                   void *workspace, int rows, int in, int out, int group, int type, int w_type, hipStream_t stream);
+size_t sample_workspace_bytes(int rows, int vocab);
+bool sample_needs(int rows, int vocab);
+xnor_status launch_sample(const void *logits, long long stride, const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                          const float *uniform, int32_t *token, float *logprob, int32_t *kept, void *workspace, int rows, int vocab, int type,
+                          hipStream_t stream);
 
 }  // namespace xnor

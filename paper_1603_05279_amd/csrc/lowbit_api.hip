@@ -9,6 +9,7 @@ using namespace xnor;
 namespace {
 
 constexpr int MAX_ROWS = 65535 * 64, MAX_WIDTH = 1 << 24, MAX_VOCAB = 1 << 30, MAX_COLS = 32768, MAX_GIVEN = 1024, MAX_TOP = 32;
+constexpr int MAX_W8_IN = 131071;          // 128 * 128 products within 31 bits
 
 template <class... P> bool aligned16(P... p) { return ((reinterpret_cast<uintptr_t>(p) | ... | 0) & 15u) == 0; }
 bool w4_group(int g) { return g == 32 || g == 64 || g == 128; }
@@ -23,6 +24,24 @@ xnor_status check_logprobs(int token_bytes, int rows, int vocab, int given, int 
     if (rows < 0 || rows > MAX_ROWS || vocab <= 0 || vocab > MAX_VOCAB || given < 0 || top < 0) return XNOR_ERR_SHAPE;
     if (given > MAX_GIVEN || top > MAX_TOP || !known_type(type) || (given && token_bytes != 4 && token_bytes != 8)) return XNOR_ERR_UNSUPPORTED;
     return XNOR_OK;
+}
+
+bool row_group(int g) { return g == 0 || w4_group(g); }
+xnor_status check_w8(int rows, int in, int out)
+{
+    if (rows < 0 || rows > MAX_ROWS || in <= 0 || out <= 0 || in > MAX_WIDTH || out > MAX_WIDTH) return XNOR_ERR_SHAPE;
+    return in > MAX_W8_IN ? XNOR_ERR_UNSUPPORTED : XNOR_OK;
+}
+xnor_status check_activation(int rows, int cols, int kept_group, int function, int gated, int type)
+{
+    if (rows < 0 || rows > MAX_ROWS || cols <= 0 || cols > MAX_WIDTH / 2) return XNOR_ERR_SHAPE;
+    if (!row_group(kept_group) || function < XNOR_RELU || function > XNOR_SILU || (gated & ~1) || !known_type(type)) return XNOR_ERR_UNSUPPORTED;
+    return XNOR_OK;
+}
+xnor_status check_gradient(int rows, int in, int out, int group, int type, int w_type)
+{
+    if (rows < 0 || rows > MAX_ROWS || in <= 0 || out <= 0 || in > MAX_WIDTH || out > MAX_WIDTH) return XNOR_ERR_SHAPE;
+    return row_group(group) && known_type(type) && known_type(w_type) ? XNOR_OK : XNOR_ERR_UNSUPPORTED;
 }
 
 }  // namespace
@@ -142,6 +161,88 @@ int xnor_logprobs_backward(const void *logits, int64_t stride, const void *token
     if (!aligned16(logits, tokens, shift, entropy, g_logprob, g_entropy, g_logits)) return XNOR_ERR_ALIGN;
     return launch_logprobs_backward(logits, stride, tokens, token_bytes, shift, entropy, g_logprob, g_entropy, g_logits, rows, vocab, given, type,
                                     (hipStream_t)hip_stream);
+}
+
+int xnor_q8_rows(const void *x, int64_t x_stride, int8_t *q, float *scale, int rows, int cols, int group, int type, void *hip_stream)
+{
+    if (rows < 0 || rows > MAX_ROWS || cols <= 0 || cols > MAX_WIDTH) return XNOR_ERR_SHAPE;
+    if (!row_group(group) || !known_type(type)) return XNOR_ERR_UNSUPPORTED;
+    if (rows == 0) return XNOR_OK;
+    if (!x || !q || !scale) return XNOR_ERR_NULL;
+    if (x_stride < cols) return XNOR_ERR_SHAPE;
+    if (!aligned16(x, q, scale)) return XNOR_ERR_ALIGN;
+    return launch_q8_rows(x, x_stride, q, scale, rows, cols, group, type, (hipStream_t)hip_stream);
+}
+
+size_t xnor_w8_linear_workspace_bytes(int rows, int in, int out) { return rows <= 0 || check_w8(rows, in, out) ? 0 : w8_linear_workspace_bytes(rows, in, out); }
+
+int xnor_w8_linear(const int8_t *q, const float *x_scale, const int8_t *w, const float *w_scale, const float *bias, void *y, void *workspace, int rows,
+                   int in, int out, int type, void *hip_stream)
+{
+    if (xnor_status s = check_w8(rows, in, out)) return s;
+    if (!known_type(type)) return XNOR_ERR_UNSUPPORTED;
+    if (rows == 0) return XNOR_OK;
+    if (!q || !x_scale || !w || !w_scale || !y || (!workspace && w8_linear_needs(rows, in, out))) return XNOR_ERR_NULL;
+    if (!aligned16(q, x_scale, w, w_scale, bias, y, workspace)) return XNOR_ERR_ALIGN;
+    return launch_w8_linear(q, x_scale, w, w_scale, bias, y, workspace, rows, in, out, type, (hipStream_t)hip_stream);
+}
+
+int xnor_activation_q8(const void *x, int64_t x_stride, void *y, int8_t *q, float *scale, int8_t *kept, float *kept_scale, int rows, int cols, int group,
+                       int kept_group, int function, int gated, int type, void *hip_stream)
+{
+    if (xnor_status s = check_activation(rows, cols, kept_group, function, gated, type)) return s;
+    if (!row_group(group)) return XNOR_ERR_UNSUPPORTED;
+    if (rows == 0) return XNOR_OK;
+    if (!x || (!y && !q && !kept) || (q && !scale) || (kept && !kept_scale)) return XNOR_ERR_NULL;
+    if (x_stride < (int64_t)cols << gated) return XNOR_ERR_SHAPE;
+    if (!aligned16(x, y, q, scale, kept, kept_scale)) return XNOR_ERR_ALIGN;
+    return launch_activation_q8(x, x_stride, y, q, scale, kept, kept_scale, rows, cols, group, kept_group, function, gated, type, (hipStream_t)hip_stream);
+}
+
+int xnor_activation_backward(const int8_t *kept, const float *kept_scale, const void *g_y, int64_t g_stride, void *g_x, int rows, int cols, int kept_group,
+                             int function, int gated, int type, void *hip_stream)
+{
+    if (xnor_status s = check_activation(rows, cols, kept_group, function, gated, type)) return s;
+    if (rows == 0) return XNOR_OK;
+    if (!kept || !kept_scale || !g_y || !g_x) return XNOR_ERR_NULL;
+    if (g_stride < cols) return XNOR_ERR_SHAPE;
+    if (!aligned16(kept, kept_scale, g_y, g_x)) return XNOR_ERR_ALIGN;
+    return launch_activation_backward(kept, kept_scale, g_y, g_stride, g_x, rows, cols, kept_group, function, gated, type, (hipStream_t)hip_stream);
+}
+
+size_t xnor_q8_weight_gradient_workspace_bytes(int rows, int in, int out, int group, int type, int w_type)
+{
+    return rows <= 0 || check_gradient(rows, in, out, group, type, w_type) ? 0 : weight_gradient_workspace_bytes(rows, in, out, group, type, w_type);
+}
+
+int xnor_q8_weight_gradient(const int8_t *q, const float *scale, const void *g_y, int64_t g_stride, void *g_w, float *g_bias, int accumulate, void *workspace,
+                            int rows, int in, int out, int group, int type, int w_type, void *hip_stream)
+{
+    if (xnor_status s = check_gradient(rows, in, out, group, type, w_type)) return s;
+    if (accumulate & ~1) return XNOR_ERR_UNSUPPORTED;
+    if (rows == 0 && accumulate) return XNOR_OK;
+    if (!g_w || (rows && (!q || !scale || !g_y || !workspace))) return XNOR_ERR_NULL;
+    if (rows && g_stride < out) return XNOR_ERR_SHAPE;
+    if (!aligned16(g_w, g_bias) || (rows && !aligned16(q, scale, g_y, workspace))) return XNOR_ERR_ALIGN;
+    return launch_weight_gradient(q, scale, g_y, g_stride, g_w, g_bias, accumulate, workspace, rows, in, out, group, type, w_type, (hipStream_t)hip_stream);
+}
+
+size_t xnor_sample_workspace_bytes(int rows, int vocab)
+{
+    return rows <= 0 || rows > MAX_ROWS || vocab <= 0 || vocab > MAX_VOCAB ? 0 : sample_workspace_bytes(rows, vocab);
+}
+
+int xnor_sample(const void *logits, int64_t stride, const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p, const float *uniform,
+                int32_t *token, float *logprob, int32_t *kept, void *workspace, int rows, int vocab, int type, void *hip_stream)
+{
+    if (rows < 0 || rows > MAX_ROWS || vocab <= 0 || vocab > MAX_VOCAB) return XNOR_ERR_SHAPE;
+    if (!known_type(type)) return XNOR_ERR_UNSUPPORTED;
+    if (rows == 0) return XNOR_OK;
+    if (!logits || !uniform || !token || (!workspace && sample_needs(rows, vocab))) return XNOR_ERR_NULL;
+    if (stride < vocab) return XNOR_ERR_SHAPE;
+    if (!aligned16(logits, temperature, top_k, top_p, min_p, uniform, token, logprob, kept, workspace)) return XNOR_ERR_ALIGN;
+    return launch_sample(logits, stride, temperature, top_k, top_p, min_p, uniform, token, logprob, kept, workspace, rows, vocab, type,
+                         (hipStream_t)hip_stream);
 }
 
 }  // extern "C"

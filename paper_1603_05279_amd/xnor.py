@@ -32,7 +32,12 @@ EXPORTS = ["xnor_words_per_pixel", "xnor_output_hw", "xnor_status_string", "xnor
            "xnor_rmsnorm_q8", "xnor_rmsnorm_backward_workspace_bytes", "xnor_rmsnorm_backward",
            "xnor_w4_quantize", "xnor_w4_wimg_bytes", "xnor_w4_pack", "xnor_w4_linear_workspace_bytes", "xnor_w4_linear",
            "xnor_w4_linear_q8",
-           "xnor_logprobs_workspace_bytes", "xnor_logprobs", "xnor_logprobs_backward"]
+           "xnor_logprobs_workspace_bytes", "xnor_logprobs", "xnor_logprobs_backward",
+           "xnor_q8_rows", "xnor_w8_linear_workspace_bytes", "xnor_w8_linear", "xnor_activation_q8", "xnor_activation_backward",
+           "xnor_q8_weight_gradient_workspace_bytes", "xnor_q8_weight_gradient", "xnor_sample_workspace_bytes", "xnor_sample"]
+
+XNOR_RELU, XNOR_GELU, XNOR_SILU = 0, 1, 2
+FUNCTIONS = {"relu": XNOR_RELU, "gelu": XNOR_GELU, "silu": XNOR_SILU}
 
 
 class XnorError(RuntimeError):
@@ -135,7 +140,16 @@ def lib():
                 ("xnor_w4_linear_q8", [vp] * 5 + [ip] * 6 + [vp], ip),
                 ("xnor_logprobs_workspace_bytes", [ip] * 3, size),
                 ("xnor_logprobs", [vp, ll, vp, ip] + [vp] * 7 + [ip] * 5 + [vp], ip),
-                ("xnor_logprobs_backward", [vp, ll, vp, ip] + [vp] * 5 + [ip] * 4 + [vp], ip)):
+                ("xnor_logprobs_backward", [vp, ll, vp, ip] + [vp] * 5 + [ip] * 4 + [vp], ip),
+                ("xnor_q8_rows", [vp, ll, vp, vp] + [ip] * 4 + [vp], ip),
+                ("xnor_w8_linear_workspace_bytes", [ip] * 3, size),
+                ("xnor_w8_linear", [vp] * 7 + [ip] * 4 + [vp], ip),
+                ("xnor_activation_q8", [vp, ll] + [vp] * 5 + [ip] * 7 + [vp], ip),
+                ("xnor_activation_backward", [vp, vp, vp, ll, vp] + [ip] * 6 + [vp], ip),
+                ("xnor_q8_weight_gradient_workspace_bytes", [ip] * 6, size),
+                ("xnor_q8_weight_gradient", [vp, vp, vp, ll, vp, vp, ip, vp] + [ip] * 6 + [vp], ip),
+                ("xnor_sample_workspace_bytes", [ip] * 2, size),
+                ("xnor_sample", [vp, ll] + [vp] * 9 + [ip] * 3 + [vp], ip)):
             getattr(L, name).argtypes = args
             getattr(L, name).restype = res
         _lib = L
@@ -353,6 +367,50 @@ def xnor_logprobs_backward(logits, tokens, shift, entropy, g_logprob, g_entropy,
     _call.xnor_logprobs_backward(logits, tokens, shift, entropy, g_logprob, g_entropy, g_logits, rows, vocab, given, stream)
 
 
+def xnor_q8_rows(x, q, scale, rows, cols, group, stream=None):
+    _call.xnor_q8_rows(x, q, scale, rows, cols, group, stream)
+
+
+def w8_linear_workspace_bytes(rows, in_features, out_features):
+    return int(lib().xnor_w8_linear_workspace_bytes(rows, in_features, out_features))
+
+
+def xnor_w8_linear(q, x_scale, w, w_scale, bias, y, workspace, rows, in_features, out_features, stream=None):
+    _call.xnor_w8_linear(q, x_scale, w, w_scale, bias, y, workspace, rows, in_features, out_features, stream)
+
+
+def _function(function):
+    return FUNCTIONS[function] if isinstance(function, str) else int(function)
+
+
+def xnor_activation_q8(x, y, q, scale, kept, kept_scale, rows, cols, group, kept_group, function, gated=False, stream=None):
+    """`function`: a name of FUNCTIONS or its number."""
+    _call.xnor_activation_q8(x, y, q, scale, kept, kept_scale, rows, cols, group, kept_group, _function(function), int(gated), stream)
+
+
+def xnor_activation_backward(kept, kept_scale, g_y, g_x, rows, cols, kept_group, function, gated=False, stream=None):
+    _call.xnor_activation_backward(kept, kept_scale, g_y, g_x, rows, cols, kept_group, _function(function), int(gated), stream)
+
+
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}      # xnor_dtype
+
+
+def q8_weight_gradient_workspace_bytes(rows, in_features, out_features, group, dtype, weight_dtype):
+    return int(lib().xnor_q8_weight_gradient_workspace_bytes(rows, in_features, out_features, group, _DTYPES[dtype], _DTYPES[weight_dtype]))
+
+
+def xnor_q8_weight_gradient(q, scale, g_y, g_w, g_bias, workspace, rows, in_features, out_features, group, accumulate=False, stream=None):
+    _call.xnor_q8_weight_gradient(q, scale, g_y, g_w, g_bias, int(accumulate), workspace, rows, in_features, out_features, group, stream)
+
+
+def sample_workspace_bytes(rows, vocab):
+    return int(lib().xnor_sample_workspace_bytes(rows, vocab))
+
+
+def xnor_sample(logits, temperature, top_k, top_p, min_p, uniform, token, logprob, kept, workspace, rows, vocab, stream=None):
+    _call.xnor_sample(logits, temperature, top_k, top_p, min_p, uniform, token, logprob, kept, workspace, rows, vocab, stream)
+
+
 def xnor_pack_weights(w, wbits, alpha, wmfma, k_out, c, kh, kw, stream=None):
     _call.xnor_pack_weights(w, wbits, alpha, wmfma, k_out, c, kh, kw, stream)
 
@@ -439,6 +497,26 @@ class W4Weights:
             zero = torch.empty((out_features, groups), dtype=torch.uint8, device=w.device) if zeros else None
         xnor_w4_quantize(w, codes, scale, zero, out_features, in_features, group, stream)
         return cls(codes, scale, zero, in_features, group, stream)
+
+
+class W8Weights:
+    """8-bit weights and their scales, one per output, as xnor_w8_linear takes them; from real weights [out][in] by xnor_q8_rows.
+
+    With a `stream` the memory is taken there, where it is written, and kept for the current stream too."""
+
+    def __init__(self, w, stream=None):
+        out_features, in_features = self.shape = tuple(w.shape)
+        with on_stream(stream):
+            self.codes = torch.empty((out_features, in_features), dtype=torch.int8, device=w.device)
+            self.scale = torch.empty((out_features,), dtype=torch.float32, device=w.device)
+        if stream is not None:
+            for t in (self.codes, self.scale):
+                t.record_stream(torch.cuda.current_stream(w.device))
+        self.quantize(w, stream)
+
+    def quantize(self, w, stream=None):
+        """New values in the same buffers."""
+        xnor_q8_rows(w, self.codes, self.scale, *self.shape, 0, stream)
 
 
 class ConvBuffers:
