@@ -2,48 +2,47 @@
 //
 //     g_w[o][k] = sum_r g[r][o] x[r][k],    x = q * scale
 // is a product of two matrices that both run along the rows, which neither stores next to each other.  Three launches:
-//   range   the largest magnitude of every column of g (and its sum, the bias' gradient) and of the scales, in parts of the rows
+//   range   the largest magnitude of every column of g (and its sum, the bias' gradient) and of the scales, in up to eight parts of the rows
 //   stage   both matrices as float16 operands of the matrix instructions, transposed, each column multiplied by the power of two that brings its largest to 2^15 (float16
 //           then holds 8- and 11-bit gradients exactly down to 2^-29 of the largest)
 //   product the sums, and the powers of two taken out again
 #include "xnor_internal.h"
 #include "lowbit.h"
-#include "w4_form.h"
+#include "tiles.h"
 #include <algorithm>
+#include <cmath>
 
 namespace xnor {
 
 namespace {
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-
-constexpr int STAGED_ROWS = 64, STAGED_COLS = 128;      // of a workgroup of the second launch
+constexpr int STAGED_ROWS = 64, STAGED_COLS = 128;      // of a workgroup of the staging launch
+constexpr int RANGE_COLS = 128, RANGE_PARTS = 8;        // of a workgroup of the first launch; of the rows, at most
 
 // Where the launches keep what they hand on:
-//   x, g     [tile of 32 columns][step of 16 rows][part][lane][16 bytes]: lane holds column lane & 31, rows 8 (lane >> 5) .. + 7 of the step; rows behind the last are 0
+//   x, g     float16 [column][part][row], rows behind the last up to a whole 64 are 0
 //   top, sum [part of the rows][columns]: largest magnitudes of g and of the scales, sums of g
 //   e        exponents of the columns of g and of the groups
 struct Places {
-    int steps, parts_x, parts_g, tiles_x, tiles_g, groups, parts, columns;
+    int padded, parts_x, parts_g, groups, parts, columns;       // padded: rows
     size_t x_at, g_at, top_at, sum_at, e_at, total;
     __host__ __device__ Places(int rows, int in, int out, int group, int type, int w_type)
     {
-        steps = (rows + STAGED_ROWS - 1) / STAGED_ROWS * (STAGED_ROWS / 16);
+        padded = (rows + STAGED_ROWS - 1) / STAGED_ROWS * STAGED_ROWS;
         parts_x = w_type == XNOR_BF16 ? 1 : 2;
         parts_g = w_type != XNOR_BF16 && type == XNOR_F32 ? 2 : 1;
-        tiles_x = (in + 31) / 32;
-        tiles_g = (out + 31) / 32;
         groups = group ? (in + group - 1) / group : 1;
         columns = (out + 3) / 4 * 4 + (groups + 3) / 4 * 4;     // (g's first, the groups from `groups_at` on)
-        const int blocks = (out + 511) / 512 + (groups + 511) / 512, wanted = (512 + blocks - 1) / blocks, most = (rows + 31) / 32;
-        parts = wanted < most ? wanted : most;
+        parts = (rows + 127) / 128 < RANGE_PARTS ? (rows + 127) / 128 : RANGE_PARTS;
         x_at = 0;
-        g_at = x_at + (size_t)tiles_x * steps * parts_x * 1024;
-        top_at = g_at + (size_t)tiles_g * steps * parts_g * 1024;
+        g_at = x_at + (size_t)in * pitch_x();
+        top_at = (g_at + (size_t)out * pitch_g() + 15) / 16 * 16;
         sum_at = top_at + (size_t)parts * columns * 4;
         e_at = sum_at + (size_t)parts * columns * 4;
         total = e_at + (size_t)columns * 4;
     }
+    __host__ __device__ uint32_t pitch_x() const { return 2u * padded * parts_x; }
+    __host__ __device__ uint32_t pitch_g() const { return 2u * padded * parts_g; }
     __host__ __device__ int groups_at(int out) const { return (out + 3) / 4 * 4; }
 };
 
@@ -58,46 +57,74 @@ struct GradArgs {
     int rows, in, out, group, type, w_type, accumulate;
 };
 
-// Largest finite magnitude and sum of 8 columns per lane; four waves take the rows of a part in turn.
-template <int TYPE> __device__ __forceinline__ void range_of(const void *m, long long stride, int rows, int cols, int block, int part, int parts, uint32_t *top, float *sum)
+// Largest finite magnitude and sum of a column: 16 lanes of 8 columns, 16 rows side by side in a workgroup of four waves, joined in LDS in one order.
+// What bounds it: the memory (2048 x 8192 bfloat16 16 us alone, 34 MB).
+template <int TYPE> __device__ __forceinline__ void range_of(const GradArgs &a, const Places &p, const void *m, long long stride, int cols, int block, bool is_g)
 {
     typedef real_t<TYPE> T;
-    __shared__ uint32_t tops[4][512];
-    __shared__ float sums[4][512];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = 512 * block + 8 * lane, n = cols - c;
-    const int first = (int)((long long)rows * part / parts), last = (int)((long long)rows * (part + 1) / parts);
+    constexpr int WAVES = 4, AT_ONCE = 8;
+    __shared__ uint32_t tops[WAVES][RANGE_COLS];
+    __shared__ float sums[WAVES][RANGE_COLS];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = RANGE_COLS * block + 8 * (lane & 15), n = cols - c;
+    const int first = (int)((long long)a.rows * blockIdx.y / p.parts), last = (int)((long long)a.rows * (blockIdx.y + 1) / p.parts);
     uint32_t t[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (int r = first + wave; r < last; r += 4) {
-        Real8<TYPE> v;
-        v.load(static_cast<const T *>(m) + (size_t)r * stride + c, n);
+    auto take = [&](const Real8<TYPE> &v) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const uint32_t bits = __float_as_uint(v[j]) & 0x7fffffffu;
             t[j] = max(t[j], bits < 0x7f800000u ? bits : 0u);
             s[j] += v[j];
         }
+    };
+    const T *from = static_cast<const T *>(m) + c;
+    int r = first + 4 * wave + (lane >> 4);
+    if (n >= 8)
+        for (; r + 4 * WAVES * (AT_ONCE - 1) < last; r += 4 * WAVES * AT_ONCE) {
+            Real8<TYPE> v[AT_ONCE];
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) v[i].load(from + (size_t)(r + 4 * WAVES * i) * stride, 8);
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) take(v[i]);
+        }
+    for (; r < last; r += 4 * WAVES) {
+        Real8<TYPE> v;
+        v.load(from + (size_t)r * stride, n);
+        take(v);
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        tops[wave][8 * lane + j] = t[j];
-        sums[wave][8 * lane + j] = s[j];
+#pragma unroll
+        for (int d = 16; d < 64; d <<= 1) {
+            t[j] = max(t[j], (uint32_t)__shfl_xor((int)t[j], d, 64));
+            s[j] += __shfl_xor(s[j], d, 64);
+        }
+        if (lane < 16) {
+            tops[wave][8 * lane + j] = t[j];
+            sums[wave][8 * lane + j] = s[j];
+        }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < 512 && 512 * block + i < cols; i += 256) {
-        top[512 * block + i] = max(max(tops[0][i], tops[1][i]), max(tops[2][i], tops[3][i]));
-        if (sum) sum[512 * block + i] = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
+    const int i = threadIdx.x, o = RANGE_COLS * block + i;
+    if (i >= RANGE_COLS || o >= cols) return;
+    uint32_t top = 0;
+    float sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        top = max(top, tops[w][i]);
+        sum += sums[w][i];
     }
+    const int at = is_g ? o : p.groups_at(a.out) + o;
+    reinterpret_cast<uint32_t *>(a.work + p.top_at)[(size_t)blockIdx.y * p.columns + at] = top;
+    if (is_g) reinterpret_cast<float *>(a.work + p.sum_at)[(size_t)blockIdx.y * p.columns + at] = sum;
 }
 
 template <int TYPE> __global__ __launch_bounds__(256) void gradient_range_kernel(GradArgs a)
 {
     const Places p(a.rows, a.in, a.out, a.group, a.type, a.w_type);
-    const int blocks_g = (a.out + 511) / 512, part = blockIdx.y;
-    uint32_t *top = reinterpret_cast<uint32_t *>(a.work + p.top_at) + (size_t)part * p.columns;
-    float *sum = reinterpret_cast<float *>(a.work + p.sum_at) + (size_t)part * p.columns;
-    if ((int)blockIdx.x < blocks_g) range_of<TYPE>(a.g, a.g_stride, a.rows, a.out, blockIdx.x, part, p.parts, top, sum);
-    else range_of<XNOR_F32>(a.scale, p.groups, a.rows, p.groups, blockIdx.x - blocks_g, part, p.parts, top + p.groups_at(a.out), nullptr);
+    const int blocks_g = (a.out + RANGE_COLS - 1) / RANGE_COLS;
+    if ((int)blockIdx.x < blocks_g) range_of<TYPE>(a, p, a.g, a.g_stride, a.out, blockIdx.x, true);
+    else range_of<XNOR_F32>(a, p, a.scale, p.groups, p.groups, blockIdx.x - blocks_g, false);
 }
 
 // 64 rows x 128 columns of one of the matrices, through LDS.
@@ -115,7 +142,8 @@ template <int TYPE> __global__ __launch_bounds__(256) void gradient_stage_kernel
         const int at = is_g ? c0 + tid : p.groups_at(a.out) + (a.group ? (c0 + tid) / a.group : 0);
         const uint32_t *top = reinterpret_cast<const uint32_t *>(a.work + p.top_at) + at;
         uint32_t most = 0;
-        for (int i = 0; i < p.parts; ++i) most = max(most, top[(size_t)i * p.columns]);
+#pragma unroll
+        for (int i = 0; i < RANGE_PARTS; ++i) most = max(most, top[(size_t)min(i, p.parts - 1) * p.columns]);
         const int e = __builtin_amdgcn_frexp_expf(__uint_as_float(most)) - (is_g ? 15 : 8);       // (an 8-bit number brings 2^7)
         exponents[tid] = e;
         if (r0 == 0) {
@@ -149,13 +177,14 @@ template <int TYPE> __global__ __launch_bounds__(256) void gradient_stage_kernel
         }
     }
     __syncthreads();
-    const int parts = is_g ? p.parts_g : p.parts_x, tiles = is_g ? p.tiles_g : p.tiles_x;
-    u32x4 *to = reinterpret_cast<u32x4 *>(a.work + (is_g ? p.g_at : p.x_at));
+    // eight lanes write the 64 rows of a column
+    const int parts = is_g ? p.parts_g : p.parts_x;
+    uint8_t *to = a.work + (is_g ? p.g_at : p.x_at);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int unit = tid + 256 * i, lane = unit & 63, step = unit >> 6 & 3, t = unit >> 8;       // (tile of the four, step of the four)
-        if (c0 / 32 + t >= tiles) break;
-        const float *from = tile + (16 * step + 8 * (lane >> 5)) * PITCH + 32 * t + (lane & 31);
+    for (int i = 0; i < STAGED_COLS * STAGED_ROWS / 8 / 256; ++i) {
+        const int unit = tid + 256 * i, col = unit >> 3, r = 8 * (unit & 7);
+        if (c0 + col >= cols) break;
+        const float *from = tile + r * PITCH + col;
         f16x8 hi, lo;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -164,69 +193,114 @@ template <int TYPE> __global__ __launch_bounds__(256) void gradient_stage_kernel
             const float rest = v - (float)hi[j];
             lo[j] = (_Float16)(__builtin_fabsf(v) < __builtin_inff() ? rest : 0.0f);
         }
-        u32x4 *at = to + (((size_t)(c0 / 32 + t) * p.steps + r0 / 16 + step) * parts) * 64 + lane;
-        at[0] = __builtin_bit_cast(u32x4, hi);
-        if (parts == 2) at[64] = __builtin_bit_cast(u32x4, lo);
+        uint8_t *at = to + ((size_t)(c0 + col) * parts * p.padded + r0 + r) * 2;
+        *reinterpret_cast<u32x4 *>(at) = __builtin_bit_cast(u32x4, hi);
+        if (parts == 2) *reinterpret_cast<u32x4 *>(at + 2 * (size_t)p.padded) = __builtin_bit_cast(u32x4, lo);
     }
 }
 
-// A wave makes 64 columns of x by 64 of g, a workgroup 128 x 128, operands straight from what was staged.
-template <int PX, int PG> __global__ __launch_bounds__(256) void gradient_product_kernel(GradArgs a)
+constexpr int TURNED = 32 * (64 * 4 + 16);          // bytes of 32 outputs x 64 inputs, outputs 16 bytes further apart
+template <class P> constexpr int lds_bytes() { return std::max(P::BUFFERS * P::BYTES, P::WAVES * TURNED); }
+
+// What bounds it: 2048 rows 4096 -> 8192, bfloat16 throughout, 125 us of 164 (a library's product of bfloat16 matrices of these sizes 116): matrix instructions and the loads of
+// their operands, which overlap in part; the others are the range (16) and the staging (22, 88 MB, 4 TB/s).  256 rows 9216 -> 4096 to float32 58 us, of which its 151 MB take 30.
+template <class P> __global__ __launch_bounds__(64 * P::WAVES) void gradient_product_kernel(GradArgs a, int blocks_x, int blocks_g)
 {
+    constexpr int WA = P::WA, TA = P::TA, TB = P::TB, WIDE = TA % 2 ? 1 : 2, PER_ROW = 8 * WIDE;           // tiles of a turn; 16-byte pieces of an output in it
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const Places p(a.rows, a.in, a.out, a.group, a.type, a.w_type);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int tx = blockIdx.x * 4 + (wave & 1) * 2, tg = blockIdx.y * 4 + (wave >> 1) * 2;
-    const f16x8 *x[2], *g[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        x[i] = reinterpret_cast<const f16x8 *>(a.work + p.x_at) + (size_t)min(tx + i, p.tiles_x - 1) * p.steps * PX * 64 + lane;
-        g[i] = reinterpret_cast<const f16x8 *>(a.work + p.g_at) + (size_t)min(tg + i, p.tiles_g - 1) * p.steps * PG * 64 + lane;
-    }
-    f32x16 acc[2][2] = {};
-    for (int s = 0; s < p.steps; ++s) {
-        f16x8 av[2][PX], bv[2][PG];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-#pragma unroll
-            for (int k = 0; k < PX; ++k) av[i][k] = x[i][((size_t)s * PX + k) * 64];
-#pragma unroll
-            for (int k = 0; k < PG; ++k) bv[i][k] = g[i][((size_t)s * PG + k) * 64];
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(av[i][0], bv[j][0], acc[i][j], 0, 0, 0);
-                if (PX == 2) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(av[i][PX - 1], bv[j][0], acc[i][j], 0, 0, 0);
-                if (PG == 2) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(av[i][0], bv[j][PG - 1], acc[i][j], 0, 0, 0);
-            }
-    }
+    int bx, bg;
+    if (!tile_of(blocks_x, blocks_g, bx, bg)) return;
+    f32x16 acc[TA][TB];
+    const Side x{a.work + p.x_at, p.pitch_x(), a.in, 2u * p.padded}, g{a.work + p.g_at, p.pitch_g(), a.out, 2u * p.padded};
+    tile_product<HalfOp, P, true, true>(acc, lds, x, g, bx * P::A, bg * P::B, 0, 2 * p.padded / P::KB, 2 * p.padded);
+    // A wave turns 32 outputs x 64 (32) inputs in LDS, so that an output's are stored next to each other.
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wx = wave % WA, wg = wave / WA;
+    uint8_t *turned = lds + wave * TURNED;
     const int *e = reinterpret_cast<const int *>(a.work + p.e_at);
+    __syncthreads();
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int o = 32 * (tg + j) + (lane & 31);
-        if (o >= a.out) continue;
-        const int eg = e[o];
+    for (int j = 0; j < TB; ++j) {
+        const int o0 = bg * P::B + (wg * TB + j) * 32, eg = e[min(o0 + (lane & 31), a.out - 1)];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int pair = 0; pair < TA; pair += WIDE) {
+            const int k0 = bx * P::A + (wx * TA + pair) * 32;
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const int k = 32 * (tx + i) + 8 * b + 4 * (lane >> 5), n = a.in - k;
-                if (n <= 0) continue;
-                const int ex = e[p.groups_at(a.out) + (a.group ? k / a.group : 0)] + eg;
-                const size_t at = (size_t)o * a.in + k;
-                f32x4 v;
+            for (int i = pair; i < pair + WIDE; ++i) {
+                const int k = k0 + (i - pair) * 32, ex = e[p.groups_at(a.out) + (a.group ? min(k, a.in - 1) / a.group : 0)] + eg;     // (groups are whole tiles)
 #pragma unroll
-                for (int m = 0; m < 4; ++m) {
-                    v[m] = __builtin_amdgcn_ldexpf(acc[i][j][4 * b + m], ex);
-                    if (a.accumulate && m < n)
-                        v[m] += a.w_type == XNOR_F32    ? static_cast<const float *>(a.g_w)[at + m]
-                                : a.w_type == XNOR_BF16 ? (float)static_cast<const __bf16 *>(a.g_w)[at + m]
-                                                        : (float)static_cast<const _Float16 *>(a.g_w)[at + m];
+                for (int b = 0; b < 4; ++b) {
+                    f32x4 v;
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) v[m] = __builtin_amdgcn_ldexpf(acc[i][j][4 * b + m], ex);
+                    *reinterpret_cast<f32x4 *>(turned + (lane & 31) * (64 * 4 + 16) + 4 * ((i - pair) * 32 + 8 * b + 4 * (lane >> 5))) = v;
                 }
-                store_four(a.g_w, a.w_type, at, v, n);
             }
+            // (a wave's own place: its lanes run in step, and what it writes there it reads itself)
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+            for (int n = 0; n < PER_ROW / 2; ++n) {
+                const int r = 64 / PER_ROW * n + lane / PER_ROW, k = 4 * (lane % PER_ROW), left = a.in - k0 - k;
+                if (o0 + r >= a.out || left <= 0) continue;
+                f32x4 v = *reinterpret_cast<const f32x4 *>(turned + r * (64 * 4 + 16) + 4 * k);
+                const size_t at = (size_t)(o0 + r) * a.in + k0 + k;
+                if (a.accumulate)
+#pragma unroll
+                    for (int m = 0; m < 4; ++m)
+                        if (m < left)
+                            v[m] += a.w_type == XNOR_F32    ? static_cast<const float *>(a.g_w)[at + m]
+                                    : a.w_type == XNOR_BF16 ? (float)static_cast<const __bf16 *>(a.g_w)[at + m]
+                                                            : (float)static_cast<const _Float16 *>(a.g_w)[at + m];
+                store_four(a.g_w, a.w_type, at, v, left);
+            }
+            asm volatile("" ::: "memory");
+        }
     }
+}
+
+template <class P> xnor_status launch_plan(const GradArgs &a, hipStream_t stream)
+{
+    constexpr unsigned lds = lds_bytes<P>();
+    const int blocks_x = (a.in + P::A - 1) / P::A, blocks_g = (a.out + P::B - 1) / P::B;
+    const long long count = (long long)blocks_x * blocks_g;
+    if (count > 0xffffff00LL / (64 * P::WAVES)) return XNOR_ERR_SHAPE;
+    auto kernel = gradient_product_kernel<P>;
+    if (hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) return XNOR_ERR_HIP;
+    kernel<<<dim3((unsigned)((count + 7) / 8 * 8)), dim3(64 * P::WAVES), lds, stream>>>(a, blocks_x, blocks_g);
+    return hip_status(hipGetLastError());
+}
+
+// Tiles of 256 x 256, 128 x 128 and 64 x 64 by their time in us, fitted to 75 products (1 to 8192 rows, 128 to 9216 inputs, 128 to 8192 outputs) for each number of parts: a
+// chunk of 64 rows takes the way to L2 and back, or where there are more tiles what L2 gives; a large tile is alone on its CU.  2048 rows 4096 -> 8192 in bfloat16 170, 187 and
+// 263 us in all; 256 rows 9216 -> 4096 65, 52, 85; 2048 rows 1024 -> 1024 78, 42, 31, with float32 results 124, 50, 35.
+int side_of(const Places &p, int in, int out, int w_bytes)
+{
+    const double chunks = p.padded / 64.0, kept = 2e-7 * in * out * w_bytes;
+    auto tiles = [&](int side) { return std::ceil((double)in / side) * std::ceil((double)out / side); };
+    const int parts = p.parts_x + p.parts_g;
+    const double small = chunks * (parts == 2   ? std::max(0.33, 0.00131 * tiles(64))
+                                   : parts == 3 ? std::max(0.5, 0.0018 * tiles(64))
+                                                : std::max(0.65, 0.0024 * tiles(64)));
+    const double middle = chunks * (parts == 2   ? std::max(0.6, 0.0023 * tiles(128))
+                                    : parts == 3 ? std::max(1.0, 0.0038 * tiles(128))
+                                                 : std::max(1.55, 0.0055 * tiles(128)));
+    const double rounds = std::ceil(tiles(256) / 256), large = rounds * (parts == 2 ? 1.6 * chunks + 10 : 3.3 * chunks + 13);
+    if (parts < 4 && large < std::min(small, middle) + kept) return 256;
+    return middle < small ? 128 : 64;
+}
+
+xnor_status launch_product(const GradArgs &a, const Places &p, hipStream_t stream)
+{
+    const int side = side_of(p, a.in, a.out, (int)type_bytes(a.w_type));
+    if (p.parts_x == 1) {
+        if (side == 256) return launch_plan<TilePlan<2, 4, 4, 2, 128, 2>>(a, stream);
+        return side == 128 ? launch_plan<TilePlan<2, 4, 2, 1, 128, 2>>(a, stream) : launch_plan<TilePlan<2, 2, 1, 1, 128, 4>>(a, stream);
+    }
+    if (p.parts_g == 1) {
+        if (side == 256) return launch_plan<TilePlan<2, 4, 4, 2, 64, 3, 2, 1>>(a, stream);
+        return side == 128 ? launch_plan<TilePlan<2, 4, 2, 1, 64, 3, 2, 1>>(a, stream) : launch_plan<TilePlan<2, 2, 1, 1, 128, 4, 2, 1>>(a, stream);
+    }
+    return side == 128 ? launch_plan<TilePlan<2, 4, 2, 1, 64, 2, 2, 2>>(a, stream) : launch_plan<TilePlan<2, 2, 1, 1, 64, 4, 2, 2>>(a, stream);
 }
 
 __global__ __launch_bounds__(256) void gradient_zero_kernel(void *g_w, float *g_bias, size_t words, bool odd, int out)
@@ -252,10 +326,8 @@ xnor_status launch_weight_gradient(const int8_t *q, const float *scale, const vo
     }
     const GradArgs a{q, scale, g_y, g_w, g_bias, static_cast<uint8_t *>(workspace), g_stride, rows, in, out, group, type, w_type, accumulate};
     const Places p(rows, in, out, group, type, w_type);
-    if ((rows + STAGED_ROWS - 1) / STAGED_ROWS > 65535 || (p.tiles_g + 3) / 4 > 65535) return XNOR_ERR_SHAPE;
-    const dim3 range((unsigned)((out + 511) / 512 + (p.groups + 511) / 512), (unsigned)p.parts);
-    const dim3 stage((unsigned)((out + STAGED_COLS - 1) / STAGED_COLS + (in + STAGED_COLS - 1) / STAGED_COLS), (unsigned)(p.steps / 4));
-    const dim3 product((unsigned)((p.tiles_x + 3) / 4), (unsigned)((p.tiles_g + 3) / 4));
+    const dim3 range((unsigned)((out + RANGE_COLS - 1) / RANGE_COLS + (p.groups + RANGE_COLS - 1) / RANGE_COLS), (unsigned)p.parts);
+    const dim3 stage((unsigned)((out + STAGED_COLS - 1) / STAGED_COLS + (in + STAGED_COLS - 1) / STAGED_COLS), (unsigned)(p.padded / STAGED_ROWS));
     xnor_status status = XNOR_OK;
     by_type(type, [&](auto t) {
         gradient_range_kernel<t()><<<range, dim3(256), 0, stream>>>(a);
@@ -265,10 +337,7 @@ xnor_status launch_weight_gradient(const int8_t *q, const float *scale, const vo
         status = hip_status(hipGetLastError());
     });
     if (status) return status;
-    if (p.parts_x == 1) gradient_product_kernel<1, 1><<<product, dim3(256), 0, stream>>>(a);
-    else if (p.parts_g == 1) gradient_product_kernel<2, 1><<<product, dim3(256), 0, stream>>>(a);
-    else gradient_product_kernel<2, 2><<<product, dim3(256), 0, stream>>>(a);
-    return hip_status(hipGetLastError());
+    return launch_product(a, p, stream);
 }
 
 }  // namespace xnor
