@@ -55,7 +55,7 @@ size_t weight_gradient_workspace_bytes(int rows, int in, int out, int group, int
 xnor_status launch_weight_gradient(const int8_t *q, const float *scale, const void *g_y, long long g_stride, void *g_w, float *g_bias, int accumulate,
                                    void *workspace, int rows, int in, int out, int group, int type, int w_type, hipStream_t stream);
 size_t sample_workspace_bytes(int rows, int vocab);
-bool sample_needs(int rows, int vocab);
+bool sample_needs(int rows, int vocab, bool top_k);
 xnor_status launch_sample(const void *logits, long long stride, const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
                           const float *uniform, int32_t *token, float *logprob, int32_t *kept, void *workspace, int rows, int vocab, int type,
                           hipStream_t stream);

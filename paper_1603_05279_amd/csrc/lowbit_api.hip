@@ -238,7 +238,7 @@ int xnor_sample(const void *logits, int64_t stride, const float *temperature, co
     if (rows < 0 || rows > MAX_ROWS || vocab <= 0 || vocab > MAX_VOCAB) return XNOR_ERR_SHAPE;
     if (!known_type(type)) return XNOR_ERR_UNSUPPORTED;
     if (rows == 0) return XNOR_OK;
-    if (!logits || !uniform || !token || (!workspace && sample_needs(rows, vocab))) return XNOR_ERR_NULL;
+    if (!logits || !uniform || !token || (!workspace && sample_needs(rows, vocab, top_k != nullptr))) return XNOR_ERR_NULL;
     if (stride < vocab) return XNOR_ERR_SHAPE;
     if (!aligned16(logits, temperature, top_k, top_p, min_p, uniform, token, logprob, kept, workspace)) return XNOR_ERR_ALIGN;
     return launch_sample(logits, stride, temperature, top_k, top_p, min_p, uniform, token, logprob, kept, workspace, rows, vocab, type,

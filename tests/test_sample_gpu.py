@@ -114,6 +114,16 @@ def test_temperatures(name, temperature):
         check(logits, u, temperature=temperature, **settings)
 
 
+@pytest.mark.parametrize("temperature", [0.02, 0.3, 1.0])
+def test_smallest_min_p(temperature):
+    """Tokens far below what weights can hold are still counted one by one."""
+    gen = generator(31)
+    logits, u = 5 * normal(gen, 12, 3000), torch.rand(12, generator=gen)
+    for least in (1e-12, 1e-14, 1e-20, 1e-30, 1e-44):
+        check(logits, u, temperature=temperature, min_p=least)
+        check(logits, u, temperature=temperature, min_p=least, top_k=2500)
+
+
 def test_greedy():
     gen = generator(22)
     logits = normal(gen, 8, 3000).bfloat16()
