@@ -57,20 +57,57 @@ __device__ __forceinline__ void to_8_bits(const float *v, uint32_t top, int8_t *
     }
 }
 
-// f and f'.  Phi(x) = erfc(-x / sqrt 2) / 2.
-template <int F> __device__ __forceinline__ float value_of(float x)
+// The root of e^(-a) for a = hi + lo >= 0, to about 1.5 units in the last place: the instruction has no results below the normal numbers, products of two roots do.
+// Its base-2 exponent is in two numbers, the second to first order.  (expf spends twice as much on ranges.)
+__device__ __forceinline__ float root_exp_minus(float hi, float lo)
 {
-    if (F == XNOR_RELU) return x > 0.0f ? x : x != x ? x : 0.0f;
-    if (F == XNOR_GELU) return x * (0.5f * erfcf(x * -0.70710678f));
-    return x / (1.0f + expf(-x));
+    constexpr float log2e = 0.721347520f, rest = 9.62981495e-9f;        // halved
+    const float t = hi * -log2e, err = __builtin_fmaf(hi, -log2e, -t) - __builtin_fmaf(lo, log2e, hi * rest);
+    const float e = __builtin_amdgcn_exp2f(t);
+    return __builtin_fmaf(e, err * 0.693147181f, e);
 }
-template <int F> __device__ __forceinline__ float slope_of(float x)
+// 1 / d for 1 <= d, one step of Newton's iteration behind the instruction's
+__device__ __forceinline__ float reciprocal(float d)
 {
-    if (F == XNOR_RELU) return x > 0.0f ? 1.0f : x != x ? x : 0.0f;
-    if (F == XNOR_GELU) return 0.5f * erfcf(x * -0.70710678f) + x * (0.39894228f * expf(-0.5f * x * x));
-    const float s = 1.0f / (1.0f + expf(-x));
-    return s * (1.0f + x * (1.0f - s));
+    const float r = __builtin_amdgcn_rcpf(d);
+    return __builtin_fmaf(r, __builtin_fmaf(-d, r, 1.0f), r);
 }
+// |x|, no farther out than where e^(-|x| / 2) is 0: times that an infinity would be NaN; a NaN stays one
+__device__ __forceinline__ float near_zero(float x)
+{
+    const float a = __builtin_fabsf(x);
+    return a > 1e4f ? 1e4f : a;
+}
+
+// f(x) and f'(x) from e^-|x| or e^(-x^2 / 2), which never overflow; a NaN stays one.
+template <int F> struct Point {
+    float value, slope;
+    __device__ __forceinline__ explicit Point(float x)
+    {
+        if (F == XNOR_RELU) {
+            value = x > 0.0f ? x : x != x ? x : 0.0f;
+            slope = x > 0.0f ? 1.0f : x != x ? x : 0.0f;
+        } else if (F == XNOR_GELU) {
+            // Phi(-|x|) = erfc(z) / 2 with z = |x| / sqrt 2;  erfc(z) e^(z^2) / t is a polynomial of t = 1 / (1 + z / 2) to 5e-8 of it (fitted to its values in 64 bits, 3e-7
+            // with float32's roundings; erfcf takes three times as long)
+            const float a = near_zero(x), square = a * a, root = root_exp_minus(0.5f * square, 0.5f * __builtin_fmaf(a, a, -square));
+            const float t = reciprocal(__builtin_fmaf(a, 0.353553391f, 1.0f));
+            constexpr float c[9] = {0.2820855975f, 0.2823898494f, 0.2429982424f, 0.2031030208f, -0.02760601416f, 0.2794856131f, -0.4884357750f, 0.2851699591f, -0.05919053033f};
+            float q = c[8];
+#pragma unroll
+            for (int i = 7; i >= 0; --i) q = __builtin_fmaf(q, t, c[i]);
+            const float part = 0.5f * root * (t * q), tail = part * root, out = a * root;
+            value = __builtin_fmaf(-out, part, __builtin_fmaxf(x, 0.0f));
+            slope = __builtin_fmaf(__builtin_copysignf(out, x), 0.398942280f * root, x >= 0.0f ? 1.0f - tail : tail);
+        } else {
+            const float a = near_zero(x), root = root_exp_minus(a, 0.0f), e = root * root, r = reciprocal(1.0f + e);
+            const float out = a * root, part = root * r;                         // |x| e^(-|x| / 2) and what makes it |x| / (1 + e^|x|)
+            value = x >= 0.0f ? x * r : -out * part;
+            slope = x >= 0.0f ? __builtin_fmaf(out * part, r, r) : __builtin_fmaf(-out * part, r, e * r);
+        }
+    }
+};
+template <int F> __device__ __forceinline__ float value_of(float x) { return Point<F>(x).value; }
 
 struct RowArgs {
     const void *x;
@@ -83,6 +120,8 @@ struct RowArgs {
 
 // A row per workgroup (blockDim.y rows of one wave each where they are narrow).  STEPS > 0: thread t holds the eight columns from 8 * (t + i * threads) on, i < STEPS;
 // STEPS = 0: rows of any width, read again once their largest is known.
+// What bounds it: the memory, with the wait for the largest between a row's reads and writes (2048 x 4096 bfloat16 8.8 us, 2.9 TB/s; 2048 x 9216 13.8 us, 4.1 TB/s), and the
+// launch below some hundred rows (7.6 us from call to call).
 template <int TYPE, int STEPS> __global__ __launch_bounds__(1024) void q8_rows_kernel(RowArgs a)
 {
     typedef real_t<TYPE> T;
@@ -162,6 +201,8 @@ template <int TYPE, int F, bool GATED> struct Act8 {
 };
 
 // The same rows through f.  kept only where the halves of a gated row are whole groups (and eights) of columns: otherwise q8_rows_kernel writes it.
+// What bounds it: the memory (2048 x 4096 bfloat16, values and kept: SiLU of gated rows 18.1 us, 3.7 TB/s; ReLU of 2048 x 9216 22.5 us, 4.2 TB/s); GELU the vector unit
+// (15.9 us, 2.6 TB/s: 19.5 us with erfcf and expf).  Gated rows whose halves are not whole groups go through both kernels: 25.7 us for 2048 x 4100.
 template <int TYPE, int F, bool GATED, int STEPS> __global__ __launch_bounds__(1024) void activation_kernel(RowArgs a)
 {
     typedef real_t<TYPE> T;
@@ -243,8 +284,7 @@ struct BackwardArgs {
     const void *g;
     void *g_x;
     long long g_stride;
-    int rows, cols, group, groups, per_row;             // groups: of a kept row; per_row: eights of a row
-    long long count;
+    int rows, cols, shift, groups, per_row;             // shift: of a column to its group (31: one for the row); groups: of a kept row; per_row: workgroups beside each other
 };
 
 // Eight neighbours of kept, widened; n: how many exist.
@@ -265,13 +305,14 @@ __device__ __forceinline__ void kept_8(const int8_t *p, int n, float *v)
     for (int j = 0; j < 8; ++j) v[j] = (float)(int8_t)(w[j / 4] >> (8 * (j & 3)));
 }
 
-// Eight columns per thread.
+// Eight columns per thread, blockDim.y rows per workgroup, so that rows and columns take no division per thread and scales none per value (both together 23.8 us instead of
+// 19.4 below).  What bounds it: the memory (2048 x 4096 bfloat16, SiLU of gated rows 19.4 us, 3.5 TB/s; GELU 14.7 us, 2.9 TB/s; ReLU of 2048 x 9216 20.1 us, 4.7 TB/s).
 template <int TYPE, int F, bool GATED> __global__ __launch_bounds__(256) void activation_grad_kernel(BackwardArgs a)
 {
     typedef real_t<TYPE> T;
-    const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (at >= a.count) return;
-    const int row = (int)(at / a.per_row), c = 8 * (int)(at - (long long)row * a.per_row), n = a.cols - c;
+    const int set = (int)(blockIdx.x / a.per_row), row = set * blockDim.y + threadIdx.y;
+    const int c = 8 * (int)((blockIdx.x - set * a.per_row) * blockDim.x + threadIdx.x), n = a.cols - c;
+    if (row >= a.rows || n <= 0) return;
     const int wide = GATED ? 2 * a.cols : a.cols;
     const int8_t *kept = a.kept + (size_t)row * wide;
     const float *scale = a.kept_scale + (size_t)row * a.groups;
@@ -280,24 +321,30 @@ template <int TYPE, int F, bool GATED> __global__ __launch_bounds__(256) void ac
     T *g_x = static_cast<T *>(a.g_x) + (size_t)row * wide;
     float x[8];
     kept_8(kept + c, n, x);
-    const float s = a.group ? scale[c / a.group] : scale[0];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] *= s;
+    const float s = scale[c >> a.shift];
     if (GATED) {
-        float up[8];
+        float up[8], su[8];
         kept_8(kept + a.cols + c, n, up);
+        if (a.cols % 8 == 0) {
+            const float all = scale[(a.cols + c) >> a.shift];           // (eights of the other half are of one group too)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) su[j] = all;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) su[j] = scale[min(a.cols + c + j, wide - 1) >> a.shift];
+        }
         Real8<TYPE> other;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float su = a.group ? scale[min(a.cols + c + j, wide - 1) / a.group] : s;
-            o.v[j] = (T)(g[j] * (up[j] * su) * slope_of<F>(x[j]));
-            other.v[j] = (T)(g[j] * value_of<F>(x[j]));
+            const Point<F> p(x[j] * s);
+            o.v[j] = (T)(g[j] * (up[j] * su[j]) * p.slope);
+            other.v[j] = (T)(g[j] * p.value);
         }
         o.store(g_x + c, n);
         other.store(g_x + a.cols + c, n);
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) o.v[j] = (T)(g[j] * slope_of<F>(x[j]));
+        for (int j = 0; j < 8; ++j) o.v[j] = (T)(g[j] * Point<F>(x[j] * s).slope);
         o.store(g_x + c, n);
     }
 }
@@ -364,12 +411,14 @@ xnor_status launch_activation_q8(const void *x, long long x_stride, void *y, int
 xnor_status launch_activation_backward(const int8_t *kept, const float *kept_scale, const void *g_y, long long g_stride, void *g_x, int rows, int cols,
                                        int kept_group, int function, int gated, int type, hipStream_t stream)
 {
-    const int per_row = (cols + 7) / 8, wide = cols << gated;
-    const BackwardArgs a{kept, kept_scale, g_y, g_x, g_stride, rows, cols, kept_group, kept_group ? (wide + kept_group - 1) / kept_group : 1, per_row,
-                         (long long)rows * per_row};
-    if (a.count >= 0xffffff00LL) return XNOR_ERR_SHAPE;
-    const dim3 grid((unsigned)((a.count + 255) / 256));
-    by_type(type, [&](auto t) { by_function(function, gated, [&](auto f, auto g) { activation_grad_kernel<t(), f(), g()><<<grid, dim3(256), 0, stream>>>(a); }); });
+    const int eights = (cols + 7) / 8, wide = cols << gated, threads = std::min((eights + 63) / 64 * 64, 256), beside = 256 / threads;
+    const int per_row = (eights + threads - 1) / threads;
+    const BackwardArgs a{kept, kept_scale, g_y, g_x, g_stride, rows, cols, kept_group ? __builtin_ctz((unsigned)kept_group) : 31,
+                         kept_group ? (wide + kept_group - 1) / kept_group : 1, per_row};
+    const long long count = (long long)((rows + beside - 1) / beside) * per_row;
+    if (count >= 0xffffff00LL / 256) return XNOR_ERR_SHAPE;
+    const dim3 grid((unsigned)count), block((unsigned)threads, (unsigned)beside);
+    by_type(type, [&](auto t) { by_function(function, gated, [&](auto f, auto g) { activation_grad_kernel<t(), f(), g()><<<grid, block, 0, stream>>>(a); }); });
     return hip_status(hipGetLastError());
 }
 
