@@ -241,8 +241,9 @@ XNOR_API int xnor_q8_weight_gradient(const int8_t *q, const float *scale, const 
  *   logprob      out  (nullable) float32 [rows]: log of the token's weight over the sum that it was drawn from
  *   kept         out  (nullable) int32 [rows]: how many tokens it was drawn from
  *   workspace         xnor_sample_workspace_bytes(rows, vocab) bytes, may be NULL where that is 0
- * Weights are held as multiples of 2^-44 (of 2^(b - 62) for a vocabulary of 2^b > 2^18) and added as integers, so that a draw depends on no order of additions and
- * differs from the formula's for a uniform within about 1e-12 of a border only.  Tokens whose weight rounds to 0 are counted, never drawn.
+ * Weights are computed to 1.5e-13 of themselves, held as multiples of 2^-44 of the largest (of 2^(b - 62) for a vocabulary of 2^b > 2^18) and added as integers, so that
+ * a draw depends on no order of additions: it is the formula's but for a uniform, a top_p or a min_p that close to a border.  Tokens whose weight rounds to 0 are
+ * counted, never drawn.
  * A row without any logit above -inf has token -1, logprob -inf and kept 0; one that holds a NaN or +inf, or whose temperature (NaN or below 0),
  * top_p, min_p or uniform is none (NaN), token -1, logprob NaN and kept 0.
  */
