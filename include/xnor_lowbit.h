@@ -220,7 +220,7 @@ XNOR_API int xnor_activation_backward(const int8_t *kept, const float *kept_scal
  * otherwise; a float32 gradient likewise; 16-bit gradients enter as they are.  Both sides are first multiplied by powers of two that bring each column's largest to 2^15,
  * and what is 2^-29 of that or less keeps its value to 2^-40 of it.  A row of g_w whose gradients hold an infinity or a NaN is not finite; neither are a group's columns
  * with a scale that is not.  The order of the sums follows from the sizes alone.
- * With rows = 0 the results are zeros (accumulate: left as they are).
+ * With rows = 0 the results are zeros (accumulate: left as they are).  in * out <= 2^35, XNOR_ERR_SHAPE otherwise.
  */
 XNOR_API size_t xnor_q8_weight_gradient_workspace_bytes(int rows, int in, int out, int group, int type, int w_type);
 XNOR_API int xnor_q8_weight_gradient(const int8_t *q, const float *scale, const void *g_y, int64_t g_stride, void *g_w, float *g_bias, int accumulate,
@@ -240,7 +240,7 @@ XNOR_API int xnor_q8_weight_gradient(const int8_t *q, const float *scale, const 
  *   token        out  int32 [rows]
  *   logprob      out  (nullable) float32 [rows]: log of the token's weight over the sum that it was drawn from
  *   kept         out  (nullable) int32 [rows]: how many tokens it was drawn from
- *   workspace         xnor_sample_workspace_bytes(rows, vocab) bytes, may be NULL where that is 0
+ *   workspace         xnor_sample_workspace_bytes(rows, vocab) bytes, may be NULL where that is 0 and with top_k
  * Weights are computed to 1.5e-13 of themselves, held as multiples of 2^-44 of the largest (of 2^(b - 62) for a vocabulary of 2^b > 2^18) and added as integers, so that
  * a draw depends on no order of additions: it is the formula's but for a uniform, a top_p or a min_p that close to a border.  Tokens whose weight rounds to 0 are
  * counted, never drawn.

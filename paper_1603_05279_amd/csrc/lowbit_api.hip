@@ -10,6 +10,7 @@ namespace {
 
 constexpr int MAX_ROWS = 65535 * 64, MAX_WIDTH = 1 << 24, MAX_VOCAB = 1 << 30, MAX_COLS = 32768, MAX_GIVEN = 1024, MAX_TOP = 32;
 constexpr int MAX_W8_IN = 131071;          // 128 * 128 products within 31 bits
+constexpr long long MAX_WEIGHTS = 1LL << 35;    // of a gradient: tiles within one launch
 
 template <class... P> bool aligned16(P... p) { return ((reinterpret_cast<uintptr_t>(p) | ... | 0) & 15u) == 0; }
 bool w4_group(int g) { return g == 32 || g == 64 || g == 128; }
@@ -40,7 +41,7 @@ xnor_status check_activation(int rows, int cols, int kept_group, int function, i
 }
 xnor_status check_gradient(int rows, int in, int out, int group, int type, int w_type)
 {
-    if (rows < 0 || rows > MAX_ROWS || in <= 0 || out <= 0 || in > MAX_WIDTH || out > MAX_WIDTH) return XNOR_ERR_SHAPE;
+    if (rows < 0 || rows > MAX_ROWS || in <= 0 || out <= 0 || in > MAX_WIDTH || out > MAX_WIDTH || (long long)in * out > MAX_WEIGHTS) return XNOR_ERR_SHAPE;
     return row_group(group) && known_type(type) && known_type(w_type) ? XNOR_OK : XNOR_ERR_UNSUPPORTED;
 }
 

@@ -262,8 +262,7 @@ template <class P> xnor_status launch_plan(const GradArgs &a, hipStream_t stream
 {
     constexpr unsigned lds = lds_bytes<P>();
     const int blocks_x = (a.in + P::A - 1) / P::A, blocks_g = (a.out + P::B - 1) / P::B;
-    const long long count = (long long)blocks_x * blocks_g;
-    if (count > 0xffffff00LL / (64 * P::WAVES)) return XNOR_ERR_SHAPE;
+    const long long count = (long long)blocks_x * blocks_g;             // (2^23 and some where they are smallest, with 256 threads each)
     auto kernel = gradient_product_kernel<P>;
     if (hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) return XNOR_ERR_HIP;
     kernel<<<dim3((unsigned)((count + 7) / 8 * 8)), dim3(64 * P::WAVES), lds, stream>>>(a, blocks_x, blocks_g);

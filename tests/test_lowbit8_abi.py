@@ -57,7 +57,7 @@ MOST = 65535 * 64
     (backward, SHAPE, dict(rows=MOST + 1)), (backward, SHAPE, dict(cols=-1)), (backward, UNSUPPORTED, dict(f=4)), (backward, UNSUPPORTED, dict(gated=3)),
     (backward, UNSUPPORTED, dict(kept_group=1)), (backward, UNSUPPORTED, dict(type=3)), (backward, ALIGN, dict(g=ODD)), (backward, ALIGN, dict(gx=ODD)),
     (backward, SHAPE, dict(rows=MOST, cols=2 ** 14, gs=2 ** 14)), (backward, 0, dict(rows=0, k=None)),
-    (gradient, NULL, dict(q=None)), (gradient, NULL, dict(s=None)), (gradient, NULL, dict(g=None)), (gradient, NULL, dict(gw=None)), (gradient, NULL, dict(work=None)),
+    (gradient, SHAPE, dict(cin=2 ** 24, out=2 ** 12, gs=2 ** 12)), (gradient, NULL, dict(q=None)), (gradient, NULL, dict(s=None)), (gradient, NULL, dict(g=None)), (gradient, NULL, dict(gw=None)), (gradient, NULL, dict(work=None)),
     (gradient, NULL, dict(rows=0, gw=None)), (gradient, SHAPE, dict(rows=-1)), (gradient, SHAPE, dict(cin=0)), (gradient, SHAPE, dict(out=0)),
     (gradient, SHAPE, dict(out=2 ** 24 + 1, gs=2 ** 25)), (gradient, SHAPE, dict(gs=3)), (gradient, UNSUPPORTED, dict(acc=2)), (gradient, UNSUPPORTED, dict(group=33)),
     (gradient, UNSUPPORTED, dict(type=3)), (gradient, UNSUPPORTED, dict(w_type=-1)), (gradient, ALIGN, dict(gw=ODD)), (gradient, ALIGN, dict(gb=ODD)),
