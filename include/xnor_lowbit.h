@@ -217,9 +217,9 @@ XNOR_API int xnor_activation_backward(const int8_t *kept, const float *kept_scal
  *   g_bias      out  (nullable) float32 [out]; accumulate as above
  *   workspace        xnor_q8_weight_gradient_workspace_bytes(rows, in, out, group, type, w_type) bytes
  * The products run on the 16-bit matrix instructions with float32 sums.  A row's value q * scale enters as one 11-bit float where w_type is XNOR_BF16, as two (22 bits)
- * otherwise; a float32 gradient likewise; 16-bit gradients enter as they are.  Both sides are first multiplied by powers of two that bring each column's largest to 2^15,
- * and what is 2^-29 of that or less keeps its value to 2^-40 of it.  A row of g_w whose gradients hold an infinity or a NaN is not finite; neither are a group's columns
- * with a scale that is not.  The order of the sums follows from the sizes alone.
+ * otherwise; a float32 gradient likewise; 16-bit gradients enter as they are.  With group 0 q enters as it is and g_y * scale as one or two such floats.  Both sides are first
+ * multiplied by powers of two that bring each column's largest to 2^15, and what is 2^-29 of that or less keeps its value to 2^-40 of it.  A row of g_w whose gradients hold an
+ * infinity or a NaN is not finite; neither are a group's columns with a scale that is not.  The order of the sums follows from the sizes alone.
  * With rows = 0 the results are zeros (accumulate: left as they are).  in * out <= 2^35, XNOR_ERR_SHAPE otherwise.
  */
 XNOR_API size_t xnor_q8_weight_gradient_workspace_bytes(int rows, int in, int out, int group, int type, int w_type);

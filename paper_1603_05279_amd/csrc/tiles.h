@@ -36,7 +36,7 @@ template <int WA_, int WB_, int TA_, int TB_, int KB_, int BUFFERS_, int PA_ = 1
     static constexpr int WA = WA_, WB = WB_, TA = TA_, TB = TB_, KB = KB_, BUFFERS = BUFFERS_;         // KB: bytes of a row in a chunk
     static constexpr int WAVES = WA * WB, A = WA * TA * 32, B = WB * TB * 32;          // rows of a workgroup's tile
     static constexpr int BYTES = (PA * A + PB * B) * KB, LOADS = BYTES / 1024 / WAVES;  // of a chunk; 1 KB loads of a wave
-    static_assert(A * KB / 1024 % WAVES == 0 && B * KB / 1024 % WAVES == 0 && PA <= 2 && PB <= PA);
+    static_assert(A * KB / 1024 % WAVES == 0 && B * KB / 1024 % WAVES == 0 && PA <= 2 && PB <= 2);
 };
 
 static __device__ const __attribute__((aligned(16))) uint8_t nothing[16] = {};          // what stands behind a row's last byte

@@ -6,6 +6,8 @@
 //   stage   both matrices as float16 operands of the matrix instructions, transposed, each column multiplied by the power of two that brings its largest to 2^15 (float16
 //           then holds 8- and 11-bit gradients exactly down to 2^-29 of the largest)
 //   product the sums, and the powers of two taken out again
+// With one scale per row the scale goes to g instead, sum_r (g[r][o] scale[r]) q[r][k], and q is an operand as it is: float32 gradients and weights then take two products of
+// parts and not three (2048 rows 4096 -> 8192 485 and 279 us).
 #include "xnor_internal.h"
 #include "lowbit.h"
 #include "tiles.h"
@@ -25,12 +27,14 @@ constexpr int RANGE_COLS = 128, RANGE_PARTS = 8;        // of a workgroup of the
 //   e        exponents of the columns of g and of the groups
 struct Places {
     int padded, parts_x, parts_g, groups, parts, columns;       // padded: rows
+    bool by_row;                                                // the scales are the rows'
     size_t x_at, g_at, top_at, sum_at, e_at, total;
     __host__ __device__ Places(int rows, int in, int out, int group, int type, int w_type)
     {
         padded = (rows + STAGED_ROWS - 1) / STAGED_ROWS * STAGED_ROWS;
-        parts_x = w_type == XNOR_BF16 ? 1 : 2;
-        parts_g = w_type != XNOR_BF16 && type == XNOR_F32 ? 2 : 1;
+        by_row = group == 0;
+        parts_x = w_type == XNOR_BF16 || by_row ? 1 : 2;
+        parts_g = w_type != XNOR_BF16 && (type == XNOR_F32 || by_row) ? 2 : 1;
         groups = group ? (in + group - 1) / group : 1;
         columns = (out + 3) / 4 * 4 + (groups + 3) / 4 * 4;     // (g's first, the groups from `groups_at` on)
         parts = (rows + 127) / 128 < RANGE_PARTS ? (rows + 127) / 128 : RANGE_PARTS;
@@ -57,9 +61,24 @@ struct GradArgs {
     int rows, in, out, group, type, w_type, accumulate;
 };
 
-// Largest finite magnitude and sum of a column: 16 lanes of 8 columns, 16 rows side by side in a workgroup of four waves, joined in LDS in one order.
+// What stands for a column's largest: where its scales are the rows', the exponent of value times scale (as an exponent, since the product may be out of float32's range),
+// otherwise the bits of the largest magnitude.  0: none that is finite and not 0.
+constexpr uint32_t EXPONENT_0 = 4096;
+__device__ __forceinline__ uint32_t size_of(float v)
+{
+    const uint32_t bits = __float_as_uint(v) & 0x7fffffffu;
+    return bits < 0x7f800000u ? bits : 0u;
+}
+__device__ __forceinline__ uint32_t size_of(float v, float scale_mant, uint32_t scale_exp)
+{
+    const float m = __builtin_fabsf(__builtin_amdgcn_frexp_mantf(v) * scale_mant);         // (0.25 .. 1)
+    const uint32_t e = (uint32_t)__builtin_amdgcn_frexp_expf(v) + scale_exp - (m < 0.5f ? 1 : 0);
+    return m > 0.0f && m < __builtin_inff() ? e : 0u;
+}
+
+// Largest size and sum of a column: 16 lanes of 8 columns, 16 rows side by side in a workgroup of four waves, joined in LDS in one order.
 // What bounds it: the memory (2048 x 8192 bfloat16 16 us alone, 34 MB).
-template <int TYPE> __device__ __forceinline__ void range_of(const GradArgs &a, const Places &p, const void *m, long long stride, int cols, int block, bool is_g)
+template <int TYPE, bool BY_ROW> __device__ __forceinline__ void range_of(const GradArgs &a, const Places &p, const void *m, long long stride, int cols, int block, bool is_g)
 {
     typedef real_t<TYPE> T;
     constexpr int WAVES = 4, AT_ONCE = 8;
@@ -69,11 +88,12 @@ template <int TYPE> __device__ __forceinline__ void range_of(const GradArgs &a, 
     const int first = (int)((long long)a.rows * blockIdx.y / p.parts), last = (int)((long long)a.rows * (blockIdx.y + 1) / p.parts);
     uint32_t t[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    auto take = [&](const Real8<TYPE> &v) {
+    auto take = [&](const Real8<TYPE> &v, float scale) {
+        const float mant = __builtin_amdgcn_frexp_mantf(scale);
+        const uint32_t exp = EXPONENT_0 + __builtin_amdgcn_frexp_expf(scale);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const uint32_t bits = __float_as_uint(v[j]) & 0x7fffffffu;
-            t[j] = max(t[j], bits < 0x7f800000u ? bits : 0u);
+            t[j] = max(t[j], BY_ROW ? size_of(v[j], mant, exp) : size_of(v[j]));
             s[j] += v[j];
         }
     };
@@ -82,15 +102,19 @@ template <int TYPE> __device__ __forceinline__ void range_of(const GradArgs &a, 
     if (n >= 8)
         for (; r + 4 * WAVES * (AT_ONCE - 1) < last; r += 4 * WAVES * AT_ONCE) {
             Real8<TYPE> v[AT_ONCE];
+            float scale[AT_ONCE];
 #pragma unroll
-            for (int i = 0; i < AT_ONCE; ++i) v[i].load(from + (size_t)(r + 4 * WAVES * i) * stride, 8);
+            for (int i = 0; i < AT_ONCE; ++i) {
+                v[i].load(from + (size_t)(r + 4 * WAVES * i) * stride, 8);
+                scale[i] = BY_ROW ? a.scale[r + 4 * WAVES * i] : 0.0f;
+            }
 #pragma unroll
-            for (int i = 0; i < AT_ONCE; ++i) take(v[i]);
+            for (int i = 0; i < AT_ONCE; ++i) take(v[i], scale[i]);
         }
     for (; r < last; r += 4 * WAVES) {
         Real8<TYPE> v;
         v.load(from + (size_t)r * stride, n);
-        take(v);
+        take(v, BY_ROW ? a.scale[r] : 0.0f);
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -123,8 +147,9 @@ template <int TYPE> __global__ __launch_bounds__(256) void gradient_range_kernel
 {
     const Places p(a.rows, a.in, a.out, a.group, a.type, a.w_type);
     const int blocks_g = (a.out + RANGE_COLS - 1) / RANGE_COLS;
-    if ((int)blockIdx.x < blocks_g) range_of<TYPE>(a, p, a.g, a.g_stride, a.out, blockIdx.x, true);
-    else range_of<XNOR_F32>(a, p, a.scale, p.groups, p.groups, blockIdx.x - blocks_g, false);
+    if ((int)blockIdx.x >= blocks_g) range_of<XNOR_F32, false>(a, p, a.scale, p.groups, p.groups, blockIdx.x - blocks_g, false);      // (not with scales of rows)
+    else if (p.by_row) range_of<TYPE, true>(a, p, a.g, a.g_stride, a.out, blockIdx.x, true);
+    else range_of<TYPE, false>(a, p, a.g, a.g_stride, a.out, blockIdx.x, true);
 }
 
 // 64 rows x 128 columns of one of the matrices, through LDS.
@@ -142,9 +167,12 @@ template <int TYPE> __global__ __launch_bounds__(256) void gradient_stage_kernel
         const int at = is_g ? c0 + tid : p.groups_at(a.out) + (a.group ? (c0 + tid) / a.group : 0);
         const uint32_t *top = reinterpret_cast<const uint32_t *>(a.work + p.top_at) + at;
         uint32_t most = 0;
+        if (is_g || !p.by_row)
 #pragma unroll
-        for (int i = 0; i < RANGE_PARTS; ++i) most = max(most, top[(size_t)min(i, p.parts - 1) * p.columns]);
-        const int e = __builtin_amdgcn_frexp_expf(__uint_as_float(most)) - (is_g ? 15 : 8);       // (an 8-bit number brings 2^7)
+            for (int i = 0; i < RANGE_PARTS; ++i) most = max(most, top[(size_t)min(i, p.parts - 1) * p.columns]);
+        int e;
+        if (p.by_row) e = !is_g ? 0 : most ? (int)(most - EXPONENT_0) - 15 : 0;
+        else e = __builtin_amdgcn_frexp_expf(__uint_as_float(most)) - (is_g ? 15 : 8);       // (an 8-bit number brings 2^7)
         exponents[tid] = e;
         if (r0 == 0) {
             reinterpret_cast<int *>(a.work + p.e_at)[at] = e;
@@ -165,12 +193,15 @@ template <int TYPE> __global__ __launch_bounds__(256) void gradient_stage_kernel
         if (is_g) {
             Real8<TYPE> v;
             v.load(static_cast<const T *>(a.g) + (size_t)(r0 + r) * a.g_stride + c0 + c, n);
+            const float scale = p.by_row && n > 0 ? a.scale[r0 + r] : 1.0f, mant = __builtin_amdgcn_frexp_mantf(scale);
+            const int exp = __builtin_amdgcn_frexp_expf(scale);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) to[j] = j < n ? __builtin_amdgcn_ldexpf(v[j], -exponents[c + j]) : 0.0f;
+            for (int j = 0; j < 8; ++j)
+                to[j] = j >= n ? 0.0f : __builtin_amdgcn_ldexpf(__builtin_amdgcn_frexp_mantf(v[j]) * mant, __builtin_amdgcn_frexp_expf(v[j]) + exp - exponents[c + j]);
         } else {
             Eight<ROWS_I8> v;
             v.load(a.q + (size_t)(r0 + r) * a.in + c0, c, n);
-            const float s = n > 0 ? a.scale[(size_t)(r0 + r) * p.groups + (a.group ? (c0 + c) / a.group : 0)] : 0.0f;
+            const float s = p.by_row ? 1.0f : n > 0 ? a.scale[(size_t)(r0 + r) * p.groups + (c0 + c) / a.group] : 0.0f;
             const float scaled = n > 0 ? __builtin_amdgcn_ldexpf(s, -exponents[c]) : 0.0f;       // (eight columns are of one group)
 #pragma unroll
             for (int j = 0; j < 8; ++j) to[j] = j < n ? (float)(int8_t)(v.w[j / 4] >> (8 * (j & 3))) * scaled : 0.0f;
@@ -203,7 +234,8 @@ constexpr int TURNED = 32 * (64 * 4 + 16);          // bytes of 32 outputs x 64 
 template <class P> constexpr int lds_bytes() { return std::max(P::BUFFERS * P::BYTES, P::WAVES * TURNED); }
 
 // What bounds it: 2048 rows 4096 -> 8192, bfloat16 throughout, 125 us of 164 (a library's product of bfloat16 matrices of these sizes 116): matrix instructions and the loads of
-// their operands, which overlap in part; the others are the range (16) and the staging (22, 88 MB, 4 TB/s).  256 rows 9216 -> 4096 to float32 58 us, of which its 151 MB take 30.
+// their operands, which overlap in part; the others are the range (16) and the staging (22, 88 MB, 4 TB/s).  256 rows 9216 -> 4096 to float32 58 us, of which its 151 MB take 30 (tiles of
+// 256 x 128, more of them in LDS or on a CU, stores past the caches or without turning: within 2 us or slower).
 template <class P> __global__ __launch_bounds__(64 * P::WAVES) void gradient_product_kernel(GradArgs a, int blocks_x, int blocks_g)
 {
     constexpr int WA = P::WA, TA = P::TA, TB = P::TB, WIDE = TA % 2 ? 1 : 2, PER_ROW = 8 * WIDE;           // tiles of a turn; 16-byte pieces of an output in it
@@ -291,6 +323,10 @@ int side_of(const Places &p, int in, int out, int w_bytes)
 xnor_status launch_product(const GradArgs &a, const Places &p, hipStream_t stream)
 {
     const int side = side_of(p, a.in, a.out, (int)type_bytes(a.w_type));
+    if (p.parts_x == 1 && p.parts_g == 2) {
+        if (side == 256) return launch_plan<TilePlan<2, 4, 4, 2, 64, 3, 1, 2>>(a, stream);
+        return side == 128 ? launch_plan<TilePlan<2, 4, 2, 1, 64, 3, 1, 2>>(a, stream) : launch_plan<TilePlan<2, 2, 1, 1, 128, 4, 1, 2>>(a, stream);
+    }
     if (p.parts_x == 1) {
         if (side == 256) return launch_plan<TilePlan<2, 4, 4, 2, 128, 2>>(a, stream);
         return side == 128 ? launch_plan<TilePlan<2, 4, 2, 1, 128, 2>>(a, stream) : launch_plan<TilePlan<2, 2, 1, 1, 128, 4>>(a, stream);
@@ -325,7 +361,8 @@ xnor_status launch_weight_gradient(const int8_t *q, const float *scale, const vo
     }
     const GradArgs a{q, scale, g_y, g_w, g_bias, static_cast<uint8_t *>(workspace), g_stride, rows, in, out, group, type, w_type, accumulate};
     const Places p(rows, in, out, group, type, w_type);
-    const dim3 range((unsigned)((out + RANGE_COLS - 1) / RANGE_COLS + (p.groups + RANGE_COLS - 1) / RANGE_COLS), (unsigned)p.parts);
+    const int scale_blocks = p.by_row ? 0 : (p.groups + RANGE_COLS - 1) / RANGE_COLS;
+    const dim3 range((unsigned)((out + RANGE_COLS - 1) / RANGE_COLS + scale_blocks), (unsigned)p.parts);
     const dim3 stage((unsigned)((out + STAGED_COLS - 1) / STAGED_COLS + (in + STAGED_COLS - 1) / STAGED_COLS), (unsigned)(p.padded / STAGED_ROWS));
     xnor_status status = XNOR_OK;
     by_type(type, [&](auto t) {

@@ -90,6 +90,48 @@ def test_gradients(rows, cin, out, name, wname):
     assert_within(g_b, d.sum(0), ((rows + 4) * EPS32 * d.abs().sum(0)).cpu(), "g_bias")
 
 
+@pytest.mark.parametrize("name,wname", [("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32"), ("f16", "f16"), ("f32", "f32")])
+def test_gradients_with_scales_of_rows_of_any_size(name, wname):
+    """Scales of 2^-140 to 2^120 on rows whose gradients are as much the other way: each product counts by its own size, wherever its factors lie."""
+    gen = generator(21)
+    rows, cin, out = 200, 140, 90
+    q, scale, g = make(gen, rows, cin, out, 0, "f32")
+    most = 10 if name == "f16" else 100
+    tilt = torch.linspace(-most, most, rows)[:, None]
+    scale, g = (scale * 2.0 ** -tilt).cuda(), (g * 2.0 ** tilt).to(TYPES[name]).cuda()
+    q = q.cuda()
+    work = filled((xnor.q8_weight_gradient_workspace_bytes(rows, cin, out, 0, TYPES[name], TYPES[wname]),), torch.uint8)
+    g_w = filled((out, cin), TYPES[wname])
+    xnor.xnor_q8_weight_gradient(q, scale, g, g_w, None, work, rows, cin, out, 0)
+    both = g.double() * scale.double()
+    total = both.abs().t().contiguous() @ q.double().abs()
+    want = both.t().contiguous() @ q.double()
+    # the product of both rounded once, kept in one or two floats of 11 bits; the sums; 2^-40 of a column's largest for each row
+    err = total * ((2.0 ** -11 if wname == "bf16" else 2.0 ** -22) * 1.001 + EPS32 + 2 * EPS32 * (rows / 16 + 18)) + 2.0 ** -39 * rows * 127 * both.abs().amax(0)[:, None]
+    bound = err + (HALF_ULP[wname] * (want.abs() + err) + SMALLEST[wname] if wname != "f32" else 0)
+    assert int((~((g_w.double() - want).abs() <= bound)).sum()) == 0
+
+
+def test_a_row_scale_that_is_not_finite_and_products_past_the_largest_number():
+    gen = generator(22)
+    rows, cin, out = 70, 50, 40
+    q, scale, g = make(gen, rows, cin, out, 0, "f32")
+    q[q == 0], g[g == 0] = 1, 1.0
+    q[3] = 0
+    q[3, 7] = -2
+    scale[3], g[3, 5] = 2.0 ** 100, 2.0 ** 100                     # (the other columns of g: 2^100 as much as before)
+    work = filled((xnor.q8_weight_gradient_workspace_bytes(rows, cin, out, 0, torch.float32, torch.float32),), torch.uint8)
+    g_w = filled((out, cin), torch.float32)
+    xnor.xnor_q8_weight_gradient(q.cuda(), scale.cuda(), g.cuda(), g_w, None, work, rows, cin, out, 0)
+    past = torch.zeros((out, cin), dtype=torch.bool)
+    past[5, 7] = True                                              # the one sum of 2^201; zeros of q leave nothing behind
+    assert torch.equal(g_w.cpu() == -float("inf"), past) and bool(g_w.cpu()[~past].isfinite().all())
+    for value in (float("inf"), float("nan")):
+        scale[3] = value
+        xnor.xnor_q8_weight_gradient(q.cuda(), scale.cuda(), g.cuda(), g_w, None, work, rows, cin, out, 0)
+        assert not bool(g_w.isfinite().any())
+
+
 def replayed(call, outputs, scratch, other):
     """What `call` leaves in `outputs`, eagerly, is what a captured one leaves each time, with eager work of `other` in the same workspaces between."""
     call()
