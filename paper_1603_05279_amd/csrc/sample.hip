@@ -20,7 +20,7 @@ constexpr int BINS = 4096, DIGITS = 2048, LIST = 1024, PER_OCTAVE = 256;
 constexpr double NO_WEIGHT = 64 * PER_OCTAVE - 1;           // in 256ths of a factor of two: from there on weights round to 0 (2^-63)
 constexpr float PER_E = 128.0f;                             // bins; the last one's tokens, 32 factors e away (2^-46), have weights that round to 0 (they have 44 bits at most)
 
-// 2^(-i / 256)
+// 2^(i / 256)
 struct Powers {
     double of[PER_OCTAVE];
     constexpr Powers() : of()
@@ -28,7 +28,7 @@ struct Powers {
         for (int i = 0; i < PER_OCTAVE; ++i) {
             const double x = i * (0x1.62e42fefa39efp-1 / PER_OCTAVE);
             double sum = 0.0;
-            for (int k = 24; k > 0; --k) sum = (sum + 1.0) * (-x / k);         // e^-x - 1 by its series, the smallest terms first
+            for (int k = 24; k > 0; --k) sum = (sum + 1.0) * (x / k);          // e^x - 1 by its series, the smallest terms first
             of[i] = 1.0 + sum;
         }
     }
@@ -48,27 +48,38 @@ struct SampleArgs {
 
 // A row's distances and weights.
 struct Weigh {
-    float top, bin_factor;
-    double factor;
-    int bits;
-    const double *table;            // 2^(-i / 256)
-    // in bins, as a real number: in 32 bits, where it never falls as the logit falls (both roundings keep the order), and that is all a bin has to do
-    __device__ __forceinline__ float bins(float l) const { return (top - l) * bin_factor; }
+    float half_top, bin_factor;
+    double top, factor, whole;
+    const double *table;            // 2^(i / 256)
+    __device__ __forceinline__ Weigh(float largest, float T, int bits, const double *powers)
+    {
+        half_top = 0.5f * largest;
+        bin_factor = fminf(2.0f * PER_E / T, 0x1.fffffep127f);
+        top = largest;
+        factor = PER_OCTAVE * 0x1.71547652b82fep+0 / (double)T;                // log2 e
+        whole = 0x1.8p52 + PER_OCTAVE * bits;
+        table = powers;
+    }
+    // in bins, as a real number: in 32 bits, where it never falls as the logit falls (both roundings keep the order), and that is all a bin has to do.  (From the halves: the
+    // distance itself may be out of range.)
+    __device__ __forceinline__ float bins(float l) const { return __builtin_fmaf(l, -0.5f, half_top) * bin_factor; }
     __device__ __forceinline__ static int bin(float b) { return (int)fminf(b, BINS - 1); }
     // in 256ths of a factor of two
-    __device__ __forceinline__ double distance(float l) const { return ((double)top - (double)l) * factor; }
-    // times 2^bits, rounded to a whole number; t as it is, or NO_WEIGHT where it is more.  Rounding and scaling by additions: their own instructions take four times as long.
-    __device__ __forceinline__ double weight(double t) const
+    __device__ __forceinline__ double distance(float l) const { return (top - (double)l) * factor; }
+    // 2^bits exp(-distance), rounded to a whole number, for a distance below NO_WEIGHT.  Rounding and scaling by additions: their own instructions take four times as long.
+    __device__ __forceinline__ double weight(float l) const
     {
-        constexpr double c = 0x1.62e42fefa39efp-9, whole = 0x1.8p52;        // ln 2 / 256
-        t = fmin(t, NO_WEIGHT);
-        const double n = t + whole, x = (n - whole) - t;
+        constexpr double c = 0x1.62e42fefa39efp-9;                              // ln 2 / 256
+        const double d = (double)l - top, n = __builtin_fma(d, factor, whole), x = __builtin_fma(d, factor, whole - n);
         const double e = __builtin_fma(x, __builtin_fma(x, __builtin_fma(x, c * c * c / 6, c * c / 2), c), 1.0);          // (the next term: 1.4e-13 at most)
-        const int i = (int)(uint32_t)__builtin_bit_cast(uint64_t, n);
-        const uint64_t w = __builtin_bit_cast(uint64_t, table[i & (PER_OCTAVE - 1)] * e) + ((uint64_t)(uint32_t)(bits - (i >> 8)) << 52);
-        return (__builtin_bit_cast(double, w) + 0x1p52) - 0x1p52;
+        const int i = (int)(uint32_t)__builtin_bit_cast(uint64_t, n);           // 256 bits - the whole 256ths
+        const uint64_t w = __builtin_bit_cast(uint64_t, table[i & (PER_OCTAVE - 1)] * e);
+        const uint32_t high = (uint32_t)(w >> 32) + ((uint32_t)(i & -PER_OCTAVE) << 12);
+        return (__builtin_bit_cast(double, (uint64_t)high << 32 | (uint32_t)w) + 0x1p52) - 0x1p52;
     }
-    __device__ __forceinline__ uint64_t whole_weight(float l) const { return (uint64_t)weight(distance(l)); }
+    // (weights are 2^44 at most: the digits behind 2^52)
+    static __device__ __forceinline__ uint64_t digits(double weight) { return __builtin_bit_cast(uint64_t, weight + 0x1p52) & 0xfffffffffffffull; }
+    __device__ __forceinline__ uint64_t whole_weight(float l) const { return distance(l) < NO_WEIGHT ? digits(weight(l)) : 0; }
 };
 
 // Largest first, of equal ones (0 and -0 among them) the lowest index first.
@@ -112,6 +123,7 @@ struct Shared : Tops {
         };
     };
     uint64_t sums[SUMS], wave_mass[16], wave_count[16];
+    uint32_t wave_tokens[16];
     uint32_t listed;
     int first[6], found_bin;
     uint64_t found_before_mass, found_before_count;
@@ -123,26 +135,53 @@ struct Place {
     uint64_t count, mass, key;
 };
 
+// Sums over the lanes up to this one: of 16 neighbours (WIDTH 16) or of the wave, without a way through LDS.
+template <int WIDTH, class T> __device__ __forceinline__ T lanes_upto(T v)
+{
+    // (lanes whose source is outside of their row, or whose row is masked, add 0)
+    const auto step = [&](auto control, auto rows) {
+        constexpr int C = decltype(control)::value, R = decltype(rows)::value;
+        if constexpr (sizeof(T) == 8) {
+            const uint32_t low = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, C, R, 0xf, false);
+            const uint32_t high = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)((uint64_t)v >> 32), C, R, 0xf, false);
+            v += (uint64_t)high << 32 | low;
+        } else {
+            v += (T)__builtin_amdgcn_update_dpp(0, (int)v, C, R, 0xf, false);
+        }
+    };
+    step(std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xf>());        // 1, 2, 4 and 8 lanes to the right
+    step(std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xf>());
+    step(std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xf>());
+    step(std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xf>());
+    if constexpr (WIDTH == 64) {
+        step(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>());    // a row's last lane to the next row (rows 1 and 3), lane 31 to the upper half
+        step(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>());
+    }
+    return v;
+}
+template <class T> __device__ __forceinline__ T lane_of(T v, int lane)
+{
+    if constexpr (sizeof(T) == 8)
+        return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+    else return (T)__builtin_amdgcn_readlane((int)v, lane);
+}
+// What the waves before this one have in their slots, and what all have.
+template <class T> __device__ __forceinline__ T waves_before(const T *slots, T &all)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const T upto = lanes_upto<16>((lane & 15) < waves ? slots[lane & 15] : (T)0);
+    all = lane_of(upto, 15);
+    return wave ? lane_of(upto, wave - 1) : (T)0;
+}
 // Sum over the threads before this one, and over all.
 __device__ __forceinline__ uint64_t scan(uint64_t v, uint64_t *slots, uint64_t &all)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    uint64_t s = v;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t o = __shfl_up((unsigned long long)s, d, 64);
-        if (lane >= d) s += o;
-    }
-    if (lane == 63) slots[wave] = s;
+    const uint64_t upto = lanes_upto<64>(v);
+    if ((threadIdx.x & 63) == 63) slots[threadIdx.x >> 6] = upto;
     __syncthreads();
-    uint64_t before = 0;
-    all = 0;
-    for (int i = 0; i < waves; ++i) {
-        if (i < wave) before += slots[i];
-        all += slots[i];
-    }
+    const uint64_t before = waves_before(slots, all);
     __syncthreads();
-    return before + s - v;
+    return before + upto - v;
 }
 
 // A row's tokens first .. last - 1.
@@ -150,7 +189,7 @@ template <int TYPE> struct Slice {
     typedef real_t<TYPE> T;
     const T *l;
     int first, last;
-    // f(eight of them, the first one's index), -inf behind the end; the next eight are on their way meanwhile, and those behind them
+    // f(eight of them, the first one's index), -inf behind the end; the next eight are on their way meanwhile
     template <class F> __device__ __forceinline__ void eights(F f) const
     {
         const int step = 8 * blockDim.x;
@@ -160,11 +199,10 @@ template <int TYPE> struct Slice {
             return v;
         };
         int c = first + 8 * (int)threadIdx.x;
-        Real8<TYPE> now = load(c), next = load(c + step);
+        Real8<TYPE> next = load(c);
         for (; c < last; c += step) {
-            const Real8<TYPE> v = now;
-            now = next;
-            next = load(c + 2 * step);
+            const Real8<TYPE> v = next;
+            next = load(c + step);
             f(v, c);
         }
     }
@@ -277,7 +315,7 @@ __device__ __forceinline__ void write_drawn(const SampleArgs &a, const Weigh &w,
     a.token[r] = (int)(uint32_t)key;
     if (a.kept) a.kept[r] = (int)count;
     // (l - top) / T - log(sum): the token's weight as it is, not as it was rounded
-    if (a.logprob) a.logprob[r] = fminf((float)(((double)logit_of(key) - (double)w.top) / (double)T - log(__builtin_ldexp((double)mass, -a.bits))), 0.0f);
+    if (a.logprob) a.logprob[r] = fminf((float)(((double)logit_of(key) - w.top) / (double)T - log(__builtin_ldexp((double)mass, -a.bits))), 0.0f);
 }
 
 __device__ __forceinline__ void make_table(Shared &s)
@@ -299,20 +337,24 @@ template <int TYPE> __device__ __forceinline__ void count_bins(Shared &s, const 
     });
     __syncthreads();
 }
-// What a bin's counts and distances stand for: weights in 2^-32, at the mean distance of its tokens (their mean weight is above that by 1 / (8 * 128^2) at most).
-__device__ __forceinline__ uint64_t estimate(uint64_t counted, int bin, int fraction)
+// What a bin's counts and distances stand for: weights in 2^-32, at the mean distance of its tokens (their mean weight is above that by 1 / (8 * 128^2) at most).  All in 32 bits.
+__device__ __forceinline__ uint64_t estimate(uint64_t counted, int bin, float step)
 {
-    const uint32_t n = (uint32_t)(counted >> 34);
-    const float within = n ? ((float)(counted & 0x3ffffffffull) / (float)n + 0.5f) / (float)(1 << fraction) : 0.0f;
-    return n ? (uint64_t)fmax((double)n * (double)exp2f((bin + within) * (-1.44269504f / PER_E)) * 0x1p32, 1.0) : 0;         // (a bin that holds any ends somewhere)
+    const float n = (float)(uint32_t)(counted >> 34);
+    const float sum = __builtin_fmaf((float)((uint32_t)(counted >> 32) & 3u), 0x1p32f, (float)(uint32_t)counted);
+    const float within = __builtin_fmaf(sum, __builtin_amdgcn_rcpf(n), 0.5f) * step;
+    const float mass = fmaxf(n * __builtin_amdgcn_exp2f(((float)bin + within) * (-1.44269504f / PER_E)) * 0x1p32f, 1.0f);          // (a bin that holds any ends somewhere)
+    const uint32_t high = (uint32_t)(mass * 0x1p-32f), low = (uint32_t)__builtin_fmaf((float)high, -0x1p32f, mass);
+    return n > 0.0f ? (uint64_t)high << 32 | low : 0;
 }
 
 // The bins' counts and masses become those of all before.  COUNTED: s.mass holds what count_bins left.
 template <bool COUNTED> __device__ __forceinline__ void add_up(Shared &s, int fraction)
 {
     constexpr int PER = 4;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    uint64_t base_c = 0, base_m = 0;
+    const float step = COUNTED ? 1.0f / (float)(1 << fraction) : 0.0f;
+    uint32_t base_c = 0;
+    uint64_t base_m = 0;
     for (int first = 0; first < BINS; first += PER * blockDim.x) {          // (once, with 1024 threads)
         const int at = first + PER * threadIdx.x;
         uint32_t c[PER], own_c = 0;
@@ -321,47 +363,32 @@ template <bool COUNTED> __device__ __forceinline__ void add_up(Shared &s, int fr
         for (int i = 0; i < PER; ++i) {
             m[i] = s.mass[at + i];
             c[i] = COUNTED ? (uint32_t)(m[i] >> 34) : s.count[at + i];
-            if (COUNTED) m[i] = estimate(m[i], at + i, fraction);
+            if (COUNTED) m[i] = estimate(m[i], at + i, step);
             own_c += c[i];
             own_m += m[i];
         }
-        uint32_t sum_c = own_c;
-        uint64_t sum_m = own_m;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t oc = __shfl_up(sum_c, d, 64);
-            const uint64_t om = __shfl_up((unsigned long long)sum_m, d, 64);
-            if (lane >= d) {
-                sum_c += oc;
-                sum_m += om;
-            }
-        }
-        if (lane == 63) {
-            s.wave_count[wave] = sum_c;
-            s.wave_mass[wave] = sum_m;
+        const uint32_t upto_c = lanes_upto<64>(own_c);
+        const uint64_t upto_m = lanes_upto<64>(own_m);
+        if ((threadIdx.x & 63) == 63) {
+            s.wave_tokens[threadIdx.x >> 6] = upto_c;
+            s.wave_mass[threadIdx.x >> 6] = upto_m;
         }
         __syncthreads();
-        uint64_t before_c = base_c + sum_c - own_c, before_m = base_m + sum_m - own_m;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            if (i >= waves) break;
-            const uint64_t wc = s.wave_count[i], wm = s.wave_mass[i];
-            if (i < wave) {
-                before_c += wc;
-                before_m += wm;
-            }
-            base_c += wc;
-            base_m += wm;
-        }
+        uint32_t all_c;
+        uint64_t all_m;
+        uint32_t before_c = base_c + waves_before(s.wave_tokens, all_c) + upto_c - own_c;
+        uint64_t before_m = base_m + waves_before(s.wave_mass, all_m) + upto_m - own_m;
+        base_c += all_c;
+        base_m += all_m;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            s.count[at + i] = (uint32_t)before_c;
+            s.count[at + i] = before_c;
             s.mass[at + i] = before_m;
             before_c += c[i];
             before_m += m[i];
         }
         if (first + PER * (int)blockDim.x >= BINS && threadIdx.x == 0) {
-            s.count[BINS] = (uint32_t)base_c;
+            s.count[BINS] = base_c;
             s.mass[BINS] = base_m;
         }
         __syncthreads();
@@ -377,6 +404,15 @@ template <class T> __device__ __forceinline__ int bin_of(const T *before, uint64
     return lo;
 }
 
+// The same by a whole wave: 64 places at a time.
+template <class T> __device__ __forceinline__ int bin_of_wide(const T *before, T target)
+{
+    static_assert(BINS == 64 * 64);
+    const int lane = threadIdx.x & 63;
+    const int block = max((int)__popcll(__ballot(before[64 * lane] < target)) - 1, 0);
+    return 64 * block + max((int)__popcll(__ballot(before[64 * block + lane] < target)) - 1, 0);
+}
+
 // In 256ths of a factor of two, the distance of weight min_p.
 __device__ __forceinline__ double furthest_of(const Settings &set)
 {
@@ -386,12 +422,11 @@ __device__ __forceinline__ double furthest_of(const Settings &set)
 __device__ __forceinline__ int list_size() { return min(LIST, (int)blockDim.x); }        // (sorted by a thread each)
 
 // From the counts and the estimated masses.  An estimate is within 1.2e-5 of the true mass (the mean distance 8e-6, float32 the rest) and half a step of the distances, so that
-// a share of the whole lies within twice that of where the estimates put it.  The even lanes look below, the odd ones above.
+// a share of the whole lies within twice that of where the estimates put it.
 __device__ __forceinline__ void make_plan(Shared &s, const Settings &set, int fraction)
 {
     if (threadIdx.x < 64) {
-        const int lane = threadIdx.x;
-        const double width = 2.4 * (1.2e-5 + 0.5 / PER_E / (1 << fraction)), away = lane & 1 ? 1 + width : 1 - width;
+        const double width = 2.4 * (1.2e-5 + 0.5 / PER_E / (1 << fraction));
         Plan p;
         p.p_first = BINS;                   // (none)
         p.p_last = p.k_first = -1;
@@ -400,14 +435,13 @@ __device__ __forceinline__ void make_plan(Shared &s, const Settings &set, int fr
         uint64_t least = s.mass[BINS], most = least;
         uint32_t wanted = 0;
         auto look = [&](double share, int &first, int &last, uint32_t &before) {
-            const int bin = min(bin_of(s.mass, (uint64_t)fmin(fmax(share * (double)(lane & 1 ? most : least) * away, 1.0), (double)most)), p.last);
-            first = __shfl(bin, 0, 64);
-            last = __shfl(bin, 1, 64);
+            first = min(bin_of_wide(s.mass, (uint64_t)fmin(fmax(share * (double)least * (1 - width), 1.0), (double)most)), p.last);
+            last = min(bin_of_wide(s.mass, (uint64_t)fmin(fmax(share * (double)most * (1 + width), 1.0), (double)most)), p.last);
             before = s.count[first];
             wanted += s.count[last + 1] - before;
         };
         if (set.top_k > 0 && (uint32_t)set.top_k < s.count[BINS]) {
-            p.last = p.k_first = bin_of(s.count, (uint64_t)set.top_k);
+            p.last = p.k_first = bin_of_wide(s.count, (uint32_t)set.top_k);
             p.k_before = s.count[p.last];
             wanted += s.count[p.last + 1] - p.k_before;
             least = s.mass[p.last];
@@ -424,9 +458,10 @@ __device__ __forceinline__ void make_plan(Shared &s, const Settings &set, int fr
             most = min((unsigned long long)most, (unsigned long long)s.mass[min(b + 2, BINS)]);
         }
         look(set.u, p.u_first, p.u_last, p.u_before);
-        const uint32_t fits = (uint32_t)list_size();
-        p.how = s.count[p.last + 1] <= fits ? LIST_ALL : wanted <= fits ? LIST_ENDS : SEARCH;
-        if (lane == 0) s.plan = p;
+        // (more than half a list takes the long sort, 10 us: 1 x 1000 float32 26 us, by its ends 14)
+        const uint32_t fits = (uint32_t)list_size(), all = s.count[p.last + 1];
+        p.how = all <= fits / 2 ? LIST_ALL : wanted <= fits / 2 ? LIST_ENDS : all <= fits ? LIST_ALL : wanted <= fits ? LIST_ENDS : SEARCH;
+        if (threadIdx.x == 0) s.plan = p;
     }
     __syncthreads();
 }
@@ -461,52 +496,59 @@ template <int TYPE> __device__ __forceinline__ void list_all(Shared &s, const Sl
 
 // Weighs a slice: the sums, and the list of what lies in the plan's bins.  A thread's sums are whole numbers below 2^52 (2^44 for each of 2^8 tokens, or 2^(62 - b)
 // for each of 2^(b - 10)), which a double holds.
-// What bounds it: vector instructions, about 40 for a token.
+// What bounds it: vector instructions, about 40 for a token, half of them of 64 bits (256 x 32000: 12 us).
 template <int TYPE> __device__ __forceinline__ void weigh(Shared &s, const Slice<TYPE> &slice, const Weigh &w, const Settings &set)
 {
     const Plan p = s.plan;
     start_list(s);
+    const bool by_count = p.k_first >= 0, by_mass = p.p_first <= p.p_last, by_weight = set.min_p > 0.0f;
     const double furthest = furthest_of(set);
-    // far tokens are weighed only where min_p is smaller than their weights
-    const float far = set.min_p > 0.0f && furthest > 40 * PER_OCTAVE ? __builtin_inff() : BINS - 1;
-    const bool by_mass = p.p_first <= p.p_last, by_weight = set.min_p > 0.0f;
-    const int k_limit = p.k_first >= 0 ? p.k_first : BINS;
-    const uint32_t u_wide = p.u_last - p.u_first, p_wide = by_mass ? p.p_last - p.p_first : 0;
+    // bins as real numbers: what is in bin i lies from i to below i + 1, in the last one from there on.  (A masked token is at an infinity or NaN, in none of them.)
+    const auto end = [](int bin) { return bin < BINS - 1 ? (float)(bin + 1) : __builtin_inff(); };
+    const float last = end(p.last), weighed = fminf(last, BINS - 1);           // (what is behind weighs nothing: where it is listed, a 0)
+    const float k_first = by_count ? (float)p.k_first : __builtin_inff(), p_first = by_mass ? (float)p.p_first : __builtin_inff(), u_first = (float)p.u_first;
+    const float p_end = end(p.p_last), u_end = end(p.u_last);
     double sum_k = 0, sum_p = 0, sum_u = 0, sum_min = 0;
     uint32_t count_min = 0;
-    slice.eights([&](const Real8<TYPE> &eight, int c) {
-        Real8<TYPE> v = eight;
-#pragma unroll 1
-        for (int pair = 0; pair < 4; ++pair) {              // (two at a time: more of them side by side leave no registers)
-bool listed[2];
-            double m[2];
+    const auto pass = [&](auto count, auto mass, auto weight) {
+        slice.eights([&](const Real8<TYPE> &v, int c) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const float l = v[j], b = w.bins(l);
-                const int bin = Weigh::bin(b);
-                const bool is = (l > -__builtin_inff()) & !(b >= far) & (bin <= p.last);
-                const double t = w.distance(l);
-                m[j] = w.weight(t);
-                m[j] = is ? m[j] : 0.0;
-                sum_k = __builtin_fma(m[j], bin < k_limit ? 1.0 : 0.0, sum_k);
-                if (by_mass) sum_p = __builtin_fma(m[j], bin < p.p_first ? 1.0 : 0.0, sum_p);
-                sum_u = __builtin_fma(m[j], bin < p.u_first ? 1.0 : 0.0, sum_u);
-                if (by_weight) {
-                    sum_min = __builtin_fma(m[j], t <= furthest ? 1.0 : 0.0, sum_min);
-                    count_min += is & (t <= furthest);
+            for (int pair = 0; pair < 4; ++pair) {              // (two at a time: more of them side by side leave no registers)
+                bool listed[2];
+                double m[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const float l = v[2 * pair + j], b = w.bins(l);
+                    m[j] = w.weight(l);
+                    m[j] = b < weighed ? m[j] : 0.0;
+                    sum_k = count() ? __builtin_fma(m[j], b < k_first ? 1.0 : 0.0, sum_k) : sum_k + m[j];
+                    if (mass()) sum_p = __builtin_fma(m[j], b < p_first ? 1.0 : 0.0, sum_p);
+                    sum_u = __builtin_fma(m[j], b < u_first ? 1.0 : 0.0, sum_u);
+                    if (weight()) {
+                        const bool is = (b < last) & (w.distance(l) <= furthest);
+                        sum_min = __builtin_fma(m[j], is ? 1.0 : 0.0, sum_min);
+                        count_min += is;
+                    }
+                    listed[j] = (b >= u_first) & (b < u_end);
+                    if (mass()) listed[j] |= (b >= p_first) & (b < p_end);
+                    if (count()) listed[j] |= (b >= k_first) & (b < last);          // (top_k's bin is the last one)
                 }
-                listed[j] = is & (((uint32_t)(bin - p.u_first) <= u_wide) | ((uint32_t)(bin - p.p_first) <= p_wide) | (bin == p.k_first));
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    if (listed[j]) {
+                        uint32_t at;
+                        if (put(s, v[2 * pair + j], c + 2 * pair + j, at)) s.list_mass[at] = Weigh::digits(m[j]);
+                    }
+                __builtin_amdgcn_sched_barrier(0);
             }
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                if (listed[j]) {
-                    uint32_t at;
-                    if (put(s, v[j], c + 2 * pair + j, at)) s.list_mass[at] = (uint64_t)m[j];
-                }
-#pragma unroll
-            for (int j = 0; j < 6; ++j) v.v[j] = v.v[j + 2];
-        }
-    });
+        });
+    };
+    // (each end that is not asked for saves 3 instructions of some 35 for a token)
+    typedef std::true_type yes;
+    typedef std::false_type no;
+    if (by_weight) pass(yes(), yes(), yes());
+    else if (by_count) by_mass ? pass(yes(), yes(), no()) : pass(yes(), no(), no());
+    else by_mass ? pass(no(), yes(), no()) : pass(no(), no(), no());
     auto add = [&](int i, uint64_t v) {
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) v += __shfl_xor((unsigned long long)v, d, 64);
@@ -522,120 +564,166 @@ bool listed[2];
     __syncthreads();
 }
 
-// The listed tokens in order, one per thread: its key and weight, and the weights of the listed ones up to it, which s.list_mass holds too.
-struct Listed {
-    uint64_t key, own, upto;
-    int n;
-    template <bool WEIGHED> __device__ __forceinline__ void sort_long(Shared &s)
-    {
-        const int i = threadIdx.x;
-        int size = 64;
-        while (size < n) size *= 2;
-        // a bitonic sort: partners within a wave by exchange of lanes, others through LDS
-        for (int k = 2; k <= size; k *= 2)
-            for (int j = k / 2; j > 0; j /= 2) {
-                uint64_t other, others = 0;
-                if (j < 64) {
-                    if (i >= size) continue;                    // (whole waves)
-                    other = __shfl_xor((unsigned long long)key, j, 64);
-                    if (WEIGHED) others = __shfl_xor((unsigned long long)own, j, 64);
-                } else {
-                    __syncthreads();
-                    s.list_key[i] = key;
-                    if (WEIGHED) s.list_mass[i] = own;
-                    __syncthreads();
-                    other = s.list_key[i ^ j];
-                    if (WEIGHED) others = s.list_mass[i ^ j];
-                }
-                const bool low = ((i & k) == 0) == ((i & j) == 0);
-                if (low ? other < key : other > key) {
-                    key = other;
-                    own = others;
-                }
+constexpr int FEW = 256;            // listed tokens that one wave takes, without waiting for the others: 2 us less than with all of them for 100
+
+// A list in order: s.list_key, and in s.list_mass the weights of the listed ones up to each.
+// Few: the first wave alone, four tokens per lane; otherwise all waves, one per thread.
+template <bool WEIGHED> __device__ __forceinline__ void sort_long(Shared &s, int n)
+{
+    const int i = threadIdx.x;
+    uint64_t key = i < n ? s.list_key[i] : ~0ull, own = WEIGHED && i < n ? s.list_mass[i] : 0;
+    int size = 64;
+    while (size < n) size *= 2;
+    // a bitonic sort: partners within a wave by exchange of lanes, others through LDS
+    for (int k = 2; k <= size; k *= 2)
+        for (int j = k / 2; j > 0; j /= 2) {
+            uint64_t other, others = 0;
+            if (j < 64) {
+                if (i >= size) continue;                    // (whole waves)
+                other = __shfl_xor((unsigned long long)key, j, 64);
+                if (WEIGHED) others = __shfl_xor((unsigned long long)own, j, 64);
+            } else {
+                __syncthreads();
+                s.list_key[i] = key;
+                if (WEIGHED) s.list_mass[i] = own;
+                __syncthreads();
+                other = s.list_key[i ^ j];
+                if (WEIGHED) others = s.list_mass[i ^ j];
             }
-    }
-    template <bool WEIGHED> __device__ __forceinline__ void sort(Shared &s, const Weigh &w)
-    {
-        const int i = threadIdx.x;
-        n = min((int)s.listed, list_size());
-        key = i < n ? s.list_key[i] : ~0ull;
-        own = WEIGHED && i < n ? s.list_mass[i] : 0;
-        if (n <= (int)blockDim.x / 2) {
-            // each token's place by counting those before it, several threads to a token (256 of 1024: 2 us, 512: 7; the sort takes 15)
-            int share = 2;
-            while (share < 64 && 2 * share * n <= (int)blockDim.x) share *= 2;
-            const int of = i / share;
-            const uint64_t mine = of < n ? s.list_key[of] : 0, its = WEIGHED && of < n ? s.list_mass[of] : 0;
-            int before = 0;
-            for (int j = i & (share - 1); j < n; j += share) before += s.list_key[j] < mine;
-            for (int d = share / 2; d > 0; d >>= 1) before += __shfl_xor(before, d, 64);
-            __syncthreads();
-            if (of < n && (i & (share - 1)) == 0) {
-                s.list_key[before] = mine;
-                if (WEIGHED) s.list_mass[before] = its;
+            const bool low = ((i & k) == 0) == ((i & j) == 0);
+            if (low ? other < key : other > key) {
+                key = other;
+                own = others;
             }
-            __syncthreads();
-            key = i < n ? s.list_key[i] : ~0ull;
-            own = WEIGHED && i < n ? s.list_mass[i] : 0;
-        } else {
-            sort_long<WEIGHED>(s);
         }
-        if (!WEIGHED && i < n) own = w.whole_weight(logit_of(key));
-        uint64_t all;
-        upto = scan(own, s.wave_mass, all) + own;
-        s.list_mass[i] = upto;
+    __syncthreads();
+    s.list_key[i] = key;
+    if (WEIGHED) s.list_mass[i] = own;
+}
+template <bool WEIGHED> __device__ __forceinline__ void sort(Shared &s, int n)
+{
+    if (n > (int)blockDim.x / 2) {
+        sort_long<WEIGHED>(s, n);
+    } else {
+        // each token's place by counting those before it, several threads to a token (256 of 1024: 2 us, 512: 7; the sort takes 15)
+        int share = 2;
+        while (share < 64 && 2 * share * n <= (int)blockDim.x) share *= 2;
+        const int of = threadIdx.x / share;
+        const uint64_t mine = of < n ? s.list_key[of] : 0, its = WEIGHED && of < n ? s.list_mass[of] : 0;
+        int before = 0;
+#pragma unroll 4
+        for (int j = threadIdx.x & (share - 1); j < n; j += share) before += s.list_key[j] < mine;
+        for (int d = share / 2; d > 0; d >>= 1) before += __shfl_xor(before, d, 64);
         __syncthreads();
+        if (of < n && (threadIdx.x & (share - 1)) == 0) {
+            s.list_key[before] = mine;
+            if (WEIGHED) s.list_mass[before] = its;
+        }
     }
-    // The first thread that says yes, LIST if none; `slot` of s.first holds LIST before.
-    __device__ __forceinline__ int first(Shared &s, bool yes, int slot) const
+    __syncthreads();
+}
+template <bool IS_FEW> struct Listed {
+    static constexpr int PER = IS_FEW ? FEW / 64 : 1;
+    uint64_t key[PER], upto[PER];
+    int first_index;
+    // (IS_FEW: of a list in order, in the first wave)
+    template <bool WEIGHED> static __device__ __forceinline__ Listed make(Shared &s, const Weigh &w, int n)
     {
-        const uint64_t all = __ballot(yes);
-        if (all && (threadIdx.x & 63) == 0) atomicMin(&s.first[slot], (int)threadIdx.x + __builtin_ctzll(all));
-        __syncthreads();
-        return s.first[slot];
+        Listed l;
+        l.first_index = PER * (int)threadIdx.x;
+        uint64_t all = 0;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const int i = l.first_index + k;
+            l.key[k] = i < n ? s.list_key[i] : ~0ull;
+            all += i >= n ? 0 : WEIGHED ? s.list_mass[i] : w.whole_weight(logit_of(l.key[k]));
+            l.upto[k] = all;
+        }
+        uint64_t whole;
+        const uint64_t before = IS_FEW ? lanes_upto<64>(all) - all : scan(all, s.wave_mass, whole);
+#pragma unroll
+        for (int k = 0; k < PER; ++k) s.list_mass[l.first_index + k] = l.upto[k] += before;
+        wait();
+        return l;
+    }
+    static __device__ __forceinline__ void wait()
+    {
+        if (IS_FEW) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");          // (what a wave writes to LDS it reads in order)
+        else __syncthreads();
+    }
+    // The first one of which f(its index, key, weights up to it) is true, LIST if none; `slot` of s.first holds LIST before.
+    template <class F> __device__ __forceinline__ int first(Shared &s, int slot, F f) const
+    {
+        if constexpr (IS_FEW) {
+            int mine = LIST;
+#pragma unroll
+            for (int k = PER - 1; k >= 0; --k) mine = f(first_index + k, key[k], upto[k]) ? first_index + k : mine;
+            const uint64_t any = __ballot(mine < LIST);
+            return any ? __builtin_amdgcn_readlane(mine, (int)__builtin_ctzll(any)) : LIST;
+        } else {
+            const uint64_t all = __ballot(f(first_index, key[0], upto[0]));
+            if (all && (threadIdx.x & 63) == 0) atomicMin(&s.first[slot], (int)threadIdx.x + __builtin_ctzll(all));
+            __syncthreads();
+            return s.first[slot];
+        }
     }
 };
 
-// From a list of all tokens that count.  False: it did not fit.
-__device__ __forceinline__ bool draw_all(const SampleArgs &a, Shared &s, const Weigh &w, const Settings &set, uint32_t seen, size_t r)
+// From a list in order of all tokens that count.
+template <bool IS_FEW> __device__ __forceinline__ void draw_listed(const SampleArgs &a, Shared &s, const Weigh &w, const Settings &set, uint32_t seen, size_t r, int n)
 {
-    if (s.listed > (uint32_t)list_size()) return false;
-    Listed l;
-    l.sort<false>(s, w);
-    const int i = threadIdx.x;
+    const Listed<IS_FEW> l = Listed<IS_FEW>::template make<false>(s, w, n);
     int count = set.top_k > 0 && (uint32_t)set.top_k < seen ? set.top_k : (int)seen;
     uint64_t mass = s.list_mass[count - 1];
-    if (set.top_p < 1.0f) count = l.first(s, i < count && l.upto >= set.top_target(mass), 0) + 1;
-    if (set.min_p > 0.0f) count = min(count, l.first(s, i >= l.n || w.distance(logit_of(l.key)) > furthest_of(set), 1));
+    if (set.top_p < 1.0f) {
+        const uint64_t target = set.top_target(mass);
+        count = l.first(s, 0, [&](int i, uint64_t, uint64_t upto) { return i < count && upto >= target; }) + 1;
+    }
+    if (set.min_p > 0.0f) {
+        const double furthest = furthest_of(set);
+        count = min(count, l.first(s, 1, [&](int i, uint64_t key, uint64_t) { return i >= n || w.distance(logit_of(key)) > furthest; }));
+    }
     mass = s.list_mass[count - 1];
-    const int at = l.first(s, l.upto >= set.draw_target(mass), 2);
-    if (i == at) write_drawn(a, w, set.T, r, l.key, count, mass);
+    const uint64_t target = set.draw_target(mass);
+    const int at = l.first(s, 2, [&](int, uint64_t, uint64_t upto) { return upto >= target; });
+    if (threadIdx.x == 0) write_drawn(a, w, set.T, r, s.list_key[at], count, mass);
+}
+// False: the list is too short.
+__device__ __forceinline__ bool draw_all(const SampleArgs &a, Shared &s, const Weigh &w, const Settings &set, uint32_t seen, size_t r)
+{
+    const int n = (int)min(s.listed, (uint32_t)LIST + 1);
+    if (n > list_size()) return false;
+    sort<false>(s, n);
+    if (n > FEW) draw_listed<false>(a, s, w, set, seen, r, n);
+    else if (threadIdx.x < 64) draw_listed<true>(a, s, w, set, seen, r, n);
     return true;
 }
 
-// From the sums and the list.  False: the plan did not hold what was looked for.
-__device__ __forceinline__ bool draw_ends(const SampleArgs &a, Shared &s, const Weigh &w, const Settings &set, uint32_t seen, size_t r)
+// From the sums and the list in order.  False: the plan did not hold what was looked for.
+template <bool IS_FEW> __device__ __forceinline__ bool draw_between(const SampleArgs &a, Shared &s, const Weigh &w, const Settings &set, uint32_t seen, size_t r, int n)
 {
-    if (s.listed > (uint32_t)list_size()) return false;
     const Plan plan = s.plan;
-    Listed l;
-    l.sort<true>(s, w);
-    const int i = threadIdx.x, bin = i < l.n ? Weigh::bin(w.bins(logit_of(l.key))) : BINS;
+    const Listed<IS_FEW> l = Listed<IS_FEW>::template make<true>(s, w, n);
     const bool by_count = plan.k_first >= 0, by_mass = plan.p_first <= plan.p_last;
     uint64_t count = seen, mass = s.sums[SUM_K];
+    const auto bin = [&](int i, uint64_t key) { return i < n ? Weigh::bin(w.bins(logit_of(key))) : BINS; };
+    const auto start_of = [&](int slot, int first) { return l.first(s, slot, [&](int i, uint64_t key, uint64_t) { return bin(i, key) >= first; }); };
     // what the listed ones before a bin's first weigh
-    auto before = [&](int first) { return first > 0 ? s.list_mass[first - 1] : 0; };
+    const auto before = [&](int first) { return first > 0 ? s.list_mass[min(first, n) - 1] : 0; };
     if (by_count) {
-        const int start = l.first(s, bin >= plan.k_first, 0), at = start + (int)(set.top_k - plan.k_before) - 1;
-        if (at >= l.n) return false;
+        const int start = start_of(0, plan.k_first), at = start + (int)(set.top_k - plan.k_before) - 1;
+        if (at >= n) return false;
         count = set.top_k;
         mass += s.list_mass[at] - before(start);
     }
     if (by_mass) {
-        const int start = l.first(s, bin >= plan.p_first, 1);
+        const int start = start_of(1, plan.p_first);
         const uint64_t base = s.sums[SUM_P] - before(start), target = set.top_target(mass);
-        const int at = l.first(s, bin >= plan.p_first && bin <= plan.p_last && base + l.upto >= target, 2);
-        if (at >= l.n || s.sums[SUM_P] >= target) return false;
+        const int at = l.first(s, 2, [&](int i, uint64_t key, uint64_t upto) {
+            const int b = bin(i, key);
+            return b >= plan.p_first && b <= plan.p_last && base + upto >= target;
+        });
+        if (at >= n || s.sums[SUM_P] >= target) return false;
         count = plan.p_before + (at - start) + 1;
         mass = base + s.list_mass[at];
     }
@@ -643,12 +731,29 @@ __device__ __forceinline__ bool draw_ends(const SampleArgs &a, Shared &s, const 
         count = min((unsigned long long)count, (unsigned long long)s.sums[COUNT_MIN]);
         mass = min((unsigned long long)mass, (unsigned long long)s.sums[SUM_MIN]);
     }
-    const int start = l.first(s, bin >= plan.u_first, 3);
+    const int start = start_of(3, plan.u_first);
     const uint64_t base = s.sums[SUM_U] - before(start), target = set.draw_target(mass);
-    const int at = l.first(s, bin >= plan.u_first && bin <= plan.u_last && base + l.upto >= target, 4);
-    if (at >= l.n || s.sums[SUM_U] >= target) return false;
-    if (i == at) write_drawn(a, w, set.T, r, l.key, count, mass);
+    const int at = l.first(s, 4, [&](int i, uint64_t key, uint64_t upto) {
+        const int b = bin(i, key);
+        return b >= plan.u_first && b <= plan.u_last && base + upto >= target;
+    });
+    if (at >= n || s.sums[SUM_U] >= target) return false;
+    if (threadIdx.x == 0) write_drawn(a, w, set.T, r, s.list_key[at], count, mass);
     return true;
+}
+// False: that, or the list is too short.
+__device__ __forceinline__ bool draw_ends(const SampleArgs &a, Shared &s, const Weigh &w, const Settings &set, uint32_t seen, size_t r)
+{
+    const int n = (int)min(s.listed, (uint32_t)LIST + 1);
+    if (n > list_size()) return false;
+    sort<true>(s, n);
+    if (n > FEW) return draw_between<false>(a, s, w, set, seen, r, n);
+    if (threadIdx.x < 64) {
+        const bool drawn = draw_between<true>(a, s, w, set, seen, r, n);
+        if (threadIdx.x == 0) s.found_bin = drawn;
+    }
+    __syncthreads();
+    return s.found_bin != 0;
 }
 
 // The first place in the order where the measure reaches the target, by itself: digit by digit of (logit, index) within its bin.
@@ -712,13 +817,12 @@ template <int TYPE, bool BY_MASS> __device__ __forceinline__ Place search(Shared
         if (Weigh::bin(w.bins(l)) == bin0 && (key & mask) == prefix) put(s, l, index, at);          // (in_bin of them: they fit)
     });
     __syncthreads();
-    Listed l;
-    l.sort<false>(s, w);
+    const int n = (int)s.listed;
+    sort<false>(s, n);
+    const Listed<false> l = Listed<false>::make<false>(s, w, n);
     const uint64_t rest = target - (BY_MASS ? before_mass : before_count);
-    const int at = l.first(s, (BY_MASS ? l.upto : (uint64_t)threadIdx.x + 1) >= rest, 0);
-    if ((int)threadIdx.x == at) s.list_key[0] = l.key;
-    __syncthreads();
-    const Place p{before_count + at + 1, before_mass + s.list_mass[at], s.list_key[0]};
+    const int at = l.first(s, 0, [&](int i, uint64_t, uint64_t upto) { return (BY_MASS ? upto : (uint64_t)i + 1) >= rest; });
+    const Place p{before_count + at + 1, before_mass + s.list_mass[at], s.list_key[at]};
     __syncthreads();
     return p;
 }
@@ -771,7 +875,7 @@ template <int TYPE> __device__ __forceinline__ void draw_searched(const SampleAr
 
 __device__ __forceinline__ Weigh weigher(const SampleArgs &a, const Shared &s, const Settings &set, float top)
 {
-    return Weigh{top, PER_E / set.T, PER_OCTAVE * 0x1.71547652b82fep+0 / (double)set.T, a.bits, s.table};          // log2 e
+    return Weigh(top, set.T, a.bits, s.table);
 }
 
 // From what a pass over the whole row left.
@@ -783,7 +887,8 @@ template <int TYPE> __device__ __forceinline__ void draw(const SampleArgs &a, Sh
 }
 
 // A row per workgroup.
-// What bounds it: vector instructions of the row's CU: 256 x 32000 bfloat16 37 us, of which 16 weigh all tokens; 23 with a top_k of 64.
+// What bounds it: the row's CU, most of all its vector instructions: 256 x 32000 bfloat16 with top_p 28 us, of which 4 read the row, 4 count it (atomics in LDS), 12 weigh all
+// tokens, 3 list and draw; 18 with a top_k of 64.
 template <int TYPE> __global__ __launch_bounds__(1024) void sample_kernel(SampleArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -828,13 +933,11 @@ template <int TYPE> __device__ __forceinline__ Slice<TYPE> slice_of(const Sample
 }
 __device__ __forceinline__ float joined_top(const SampleArgs &a, const Part *parts)
 {
-    float top = -__builtin_inff();
-    bool bad = false;
-    for (int i = 0; i < a.parts; ++i) {
-        const float t = parts[i].top;
-        bad |= t != t;
-        top = fmaxf(top, t);
-    }
+    // (a lane for each part: one after another they cost the way to memory each)
+    float top = parts[min((int)(threadIdx.x & 63), a.parts - 1)].top;
+    const bool bad = __any(top != top);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
     return bad ? __builtin_nanf("") : top;
 }
 // a row that has more than one token to draw from
@@ -874,7 +977,7 @@ template <int TYPE> __global__ __launch_bounds__(1024) void sample_weigh_kernel(
     // the bins of all parts: four of them per thread
     for (int i = 4 * threadIdx.x; i < BINS; i += 4 * blockDim.x) {
         uint64_t sum[4] = {0, 0, 0, 0};
-#pragma unroll 4
+#pragma unroll 8
         for (int p = 0; p < a.parts; ++p) {
             const uint4 v = *reinterpret_cast<const uint4 *>(parts[p].bins + i);
             const uint32_t of[4] = {v.x, v.y, v.z, v.w};
@@ -918,30 +1021,29 @@ template <int TYPE> __global__ __launch_bounds__(1024) void sample_draw_kernel(S
     make_table(s);
     start_list(s);
     // a wave copies the list of a part behind those of the parts before
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint32_t before = 0;
-    for (int p = 0; p < a.parts; ++p) {
-        const uint32_t n = parts[p].listed;
-        if (p % 16 == wave && before + n <= LIST)
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const uint32_t own = lane < a.parts ? min(parts[lane].listed, (uint32_t)(LIST + 1)) : 0, upto = lanes_upto<64>(own);
+    for (int p = wave; p < a.parts; p += waves) {
+        const uint32_t n = lane_of(own, p), before = lane_of(upto, p) - n;
+        if (before + n <= LIST)
             for (uint32_t i = lane; i < n; i += 64) {
                 s.list_key[before + i] = parts[p].list_key[i];
                 s.list_mass[before + i] = parts[p].list_mass[i];
             }
-        before = min(before + n, (uint32_t)(LIST + 1));
     }
-    if (threadIdx.x < SUMS)
-        for (int p = 0; p < a.parts; ++p) s.sums[threadIdx.x] += parts[p].sums[threadIdx.x];
+    if ((int)threadIdx.x < SUMS * a.parts)
+        atomicAdd((unsigned long long *)&s.sums[threadIdx.x % SUMS], (unsigned long long)parts[threadIdx.x / SUMS].sums[threadIdx.x % SUMS]);
     if (threadIdx.x == 0) {
-        s.listed = before;
+        s.listed = lane_of(upto, 63);
         s.plan = parts[0].plan;
     }
     __syncthreads();
     draw(a, s, row, weigher(a, s, set, top), set, parts[0].seen, r);
 }
 
-// Parts of a row (1: a row per workgroup): of 8000 tokens or so, for few rows of long vocabularies.  A workgroup takes 0.55 us for 1000 tokens that are all weighed, its parts
-// 4 launches.  In one and in parts: 1 x 128000 bfloat16 83 and 48 us, 8 x 128000 95 and 64, 16 x 64000 54 and 50, 1 x 32000 34 and 34, 64 x 64000 63 and 77.
-// With top_k few are weighed: 40 and 43, 41 and 45, 29 and 37, 21 and 29.
+// Parts of a row (1: a row per workgroup): of 8000 tokens or so, for few rows of long vocabularies.  A workgroup takes 0.4 us for 1000 tokens that are all weighed, its parts
+// 4 launches.  In one and in parts, with top_p: 1 x 128000 bfloat16 72 and 37 us, 8 x 128000 66 and 49, 16 x 64000 41 and 37, 1 x 32000 26 and 27, 64 x 64000 46 and 66.
+// With top_k few are weighed: 40 and 43 (1 x 128000), 29 and 37, 21 and 29.
 int row_parts(int rows, int vocab, bool top_k)
 {
     const int parts = (vocab + PART_TOKENS - 1) / PART_TOKENS;

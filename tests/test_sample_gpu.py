@@ -229,3 +229,26 @@ def test_rows_past_32_bits_of_offset():
 def test_no_rows():
     e = torch.empty((0, 64), device="cuda")
     xnor.xnor_sample(e, None, None, None, None, None, None, None, None, None, 0, 64)
+
+
+@pytest.mark.parametrize("rows,vocab", [(6, 2000), (2, 60000)])
+@pytest.mark.parametrize("temperature", [1e38, 3.0e37, 1e36, float("inf")])
+def test_logits_whose_distance_is_past_the_largest_number(rows, vocab, temperature):
+    """At temperatures as large as the logits every token weighs, those too whose distance to the largest float32 does not hold."""
+    gen = generator(31)
+    logits = (torch.rand(rows, vocab, generator=gen) * 2 - 1) * 3.4e38
+    logits[:, 5], logits[:, 7], logits[:, 11] = 3.4e38, -3.4e38, -float("inf")
+    uniform = torch.linspace(0.001, 0.999, rows)
+    check(logits, uniform, temperature=temperature)
+    check(logits, uniform, temperature=temperature, top_p=0.7)
+    check(logits, uniform, temperature=temperature, min_p=0.01, top_k=vocab // 2)
+
+
+@pytest.mark.parametrize("temperature", [1e-38, 1e-42, 1e-45])
+def test_the_smallest_temperatures(temperature):
+    """Logits as close to each other as the temperature is small, and others."""
+    gen = generator(32)
+    close = torch.randint(0, 6, (5, 3000), generator=gen).float() * 1e-44
+    uniform = torch.linspace(0.01, 0.99, 5)
+    check(close, uniform, temperature=temperature)
+    check(normal(gen, 5, 3000), uniform, temperature=temperature, top_p=0.5)
