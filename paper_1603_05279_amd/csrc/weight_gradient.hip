@@ -234,8 +234,9 @@ constexpr int TURNED = 32 * (64 * 4 + 16);          // bytes of 32 outputs x 64 
 template <class P> constexpr int lds_bytes() { return std::max(P::BUFFERS * P::BYTES, P::WAVES * TURNED); }
 
 // What bounds it: 2048 rows 4096 -> 8192, bfloat16 throughout, 125 us of 164 (a library's product of bfloat16 matrices of these sizes 116): matrix instructions and the loads of
-// their operands, which overlap in part; the others are the range (16) and the staging (22, 88 MB, 4 TB/s).  256 rows 9216 -> 4096 to float32 58 us, of which its 151 MB take 30 (tiles of
-// 256 x 128, more of them in LDS or on a CU, stores past the caches or without turning: within 2 us or slower).
+// their operands, which overlap in part; the others are the range (16) and the staging (22, 88 MB, 4 TB/s).  256 rows 9216 -> 4096 to float32 58 us: 32 with
+// the first chunk alone (151 MB of results), 4 more for each of the other seven (57 MB out of L2), which the results hardly hide (tiles of 256 x 128, more of them in LDS or on a CU,
+// waves of two priorities, stores past the caches or without turning: 3 us at most).
 template <class P> __global__ __launch_bounds__(64 * P::WAVES) void gradient_product_kernel(GradArgs a, int blocks_x, int blocks_g)
 {
     constexpr int WA = P::WA, TA = P::TA, TB = P::TB, WIDE = TA % 2 ? 1 : 2, PER_ROW = 8 * WIDE;           // tiles of a turn; 16-byte pieces of an output in it
