@@ -917,14 +917,14 @@ template <int TYPE> __global__ __launch_bounds__(1024) void sample_kernel(Sample
 
 // Few rows: a row in parts of at most 2^13 - 8 tokens, each in a workgroup of its own, and a launch for each step.  What a part leaves for the next:
 struct Part {
-    uint32_t bins[BINS];            // count in the upper 13 bits, the sum of 6-bit distances within the bin below
+    uint32_t bins[BINS];            // count in the upper 13 bits, the mean distance within the bin in the 19 below
     uint64_t list_key[LIST], list_mass[LIST], sums[SUMS];
     float top;
     uint32_t listed, seen;          // seen, plan: of the first part only, for the row
     Plan plan;
 };
-constexpr int PART_FRACTION = 6, PART_SHIFT = 19, PART_TOKENS = 8184, MOST_PARTS = 32, MOST_WORKGROUPS = 128;
-static_assert(PART_TOKENS < 1 << (32 - PART_SHIFT) && PART_TOKENS << PART_FRACTION < 1 << PART_SHIFT);
+constexpr int PART_FRACTION = 12, MEAN_BITS = 19, PART_TOKENS = 8184, MOST_PARTS = 32, MOST_WORKGROUPS = 256;
+static_assert(PART_TOKENS < 1 << (32 - MEAN_BITS) && (uint64_t)MOST_PARTS * PART_TOKENS << PART_FRACTION < 1ull << 32);
 
 template <int TYPE> __device__ __forceinline__ Slice<TYPE> slice_of(const SampleArgs &a, size_t r, int part)
 {
@@ -961,7 +961,12 @@ template <int TYPE> __global__ __launch_bounds__(1024) void sample_count_kernel(
     const float top = joined_top(a, parts);
     if (!is_open(set, top)) return;
     count_bins(s, slice_of<TYPE>(a, r, blockIdx.x), weigher(a, s, set, top), PART_FRACTION);
-    for (int i = threadIdx.x; i < BINS; i += blockDim.x) parts[blockIdx.x].bins[i] = (uint32_t)(s.mass[i] >> 34) << PART_SHIFT | (uint32_t)(s.mass[i] & ((1u << PART_SHIFT) - 1));
+    for (int i = threadIdx.x; i < BINS; i += blockDim.x) {
+        const uint32_t n = (uint32_t)(s.mass[i] >> 34);
+        const float mean = (float)(uint32_t)s.mass[i] / (float)max(n, 1u);             // (a part's sums are below 2^32)
+        const uint32_t its = min((uint32_t)(mean * (1 << (MEAN_BITS - PART_FRACTION)) + 0.5f), (1u << MEAN_BITS) - 1);
+        parts[blockIdx.x].bins[i] = n << MEAN_BITS | its;
+    }
 }
 
 template <int TYPE> __global__ __launch_bounds__(1024) void sample_weigh_kernel(SampleArgs a)
@@ -974,22 +979,31 @@ template <int TYPE> __global__ __launch_bounds__(1024) void sample_weigh_kernel(
     const float top = joined_top(a, parts);
     if (!is_open(set, top)) return;
     make_table(s);
-    // the bins of all parts: four of them per thread
+    // the bins of all parts: four of them per thread, eight parts on their way at once
     for (int i = 4 * threadIdx.x; i < BINS; i += 4 * blockDim.x) {
-        uint64_t sum[4] = {0, 0, 0, 0};
-#pragma unroll 8
-        for (int p = 0; p < a.parts; ++p) {
-            const uint4 v = *reinterpret_cast<const uint4 *>(parts[p].bins + i);
-            const uint32_t of[4] = {v.x, v.y, v.z, v.w};
+        uint32_t count[4] = {0, 0, 0, 0}, within[4] = {0, 0, 0, 0};
+        for (int first = 0; first < a.parts; first += 8) {
+            uint4 v[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) sum[j] += (uint64_t)(of[j] >> PART_SHIFT) << 34 | (of[j] & ((1u << PART_SHIFT) - 1));
+            for (int p = 0; p < 8; ++p) v[p] = *reinterpret_cast<const uint4 *>(parts[min(first + p, a.parts - 1)].bins + i);
+#pragma unroll
+            for (int p = 0; p < 8; ++p) {
+                const uint32_t of[4] = {v[p].x, v[p].y, v[p].z, v[p].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t its = first + p < a.parts ? of[j] : 0;
+                    const uint32_t n = its >> MEAN_BITS;
+                    count[j] += n;
+                    within[j] += n * (its & ((1u << MEAN_BITS) - 1)) >> (MEAN_BITS - PART_FRACTION);
+                }
+            }
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s.mass[i + j] = sum[j];
+        for (int j = 0; j < 4; ++j) s.mass[i + j] = (uint64_t)count[j] << 34 | within[j];
     }
     __syncthreads();
     add_up<true>(s, PART_FRACTION);
-    make_plan(s, set, PART_FRACTION);
+    make_plan(s, set, PART_FRACTION - 1);          // (means and products of them are rounded: another half of a step)
     const Slice<TYPE> slice = slice_of<TYPE>(a, r, blockIdx.x);
     const Weigh w = weigher(a, s, set, top);
     if (s.plan.how == LIST_ALL) list_all(s, slice, w);
@@ -1042,8 +1056,8 @@ template <int TYPE> __global__ __launch_bounds__(1024) void sample_draw_kernel(S
 }
 
 // Parts of a row (1: a row per workgroup): of 8000 tokens or so, for few rows of long vocabularies.  A workgroup takes 0.4 us for 1000 tokens that are all weighed, its parts
-// 4 launches.  In one and in parts, with top_p: 1 x 128000 bfloat16 72 and 37 us, 8 x 128000 66 and 49, 16 x 64000 41 and 37, 1 x 32000 26 and 27, 64 x 64000 46 and 66.
-// With top_k few are weighed: 40 and 43 (1 x 128000), 29 and 37, 21 and 29.
+// 4 launches.  In one and in parts, with top_p: 1 x 128000 bfloat16 66 and 32 us, 16 x 128000 74 and 45, 1 x 41000 30 and 28, 24 x 64000 42 and 37, 1 x 32000 26 and 28, 32 x 50000
+// 35 and 37, 64 x 64000 46 and 66.  With top_k few are weighed: 40 and 43 (1 x 128000), 29 and 37, 21 and 29.
 int row_parts(int rows, int vocab, bool top_k)
 {
     const int parts = (vocab + PART_TOKENS - 1) / PART_TOKENS;

@@ -197,7 +197,7 @@ def test_draws_of_fewer_rows_in_a_workspace_of_more():
     logits, uniform = (2 * normal(gen, 100, vocab)).cuda(), torch.rand(100, generator=gen).cuda()
     space, work = guarded(xnor.sample_workspace_bytes(100, vocab))
     want = None
-    for rows in (100, 17, 16, 15, 2, 1):
+    for rows in (100, 33, 32, 31, 17, 16, 15, 2, 1):
         assert xnor.sample_workspace_bytes(rows, vocab) <= xnor.sample_workspace_bytes(100, vocab)
         token, kept = filled((rows,), torch.int32), filled((rows,), torch.int32)
         xnor.xnor_sample(logits, None, None, torch.full((rows,), 0.9, device="cuda"), None, uniform, token, None, kept, work, rows, vocab)
