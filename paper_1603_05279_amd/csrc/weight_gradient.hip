@@ -312,7 +312,7 @@ int side_of(const Places &p, int in, int out, int w_bytes)
     const int parts = p.parts_x + p.parts_g;
     const double small = chunks * (parts == 2   ? std::max(0.33, 0.00131 * tiles(64))
                                    : parts == 3 ? std::max(0.5, 0.0018 * tiles(64))
-                                                : std::max(0.65, 0.0024 * tiles(64)));
+                                                : std::max(0.65, 0.0019 * tiles(64)));
     const double middle = chunks * (parts == 2   ? std::max(0.6, 0.0023 * tiles(128))
                                     : parts == 3 ? std::max(1.0, 0.0038 * tiles(128))
                                                  : std::max(1.55, 0.0055 * tiles(128)));
@@ -336,7 +336,7 @@ xnor_status launch_product(const GradArgs &a, const Places &p, hipStream_t strea
         if (side == 256) return launch_plan<TilePlan<2, 4, 4, 2, 64, 3, 2, 1>>(a, stream);
         return side == 128 ? launch_plan<TilePlan<2, 4, 2, 1, 64, 3, 2, 1>>(a, stream) : launch_plan<TilePlan<2, 2, 1, 1, 128, 4, 2, 1>>(a, stream);
     }
-    return side == 128 ? launch_plan<TilePlan<2, 4, 2, 1, 64, 2, 2, 2>>(a, stream) : launch_plan<TilePlan<2, 2, 1, 1, 64, 4, 2, 2>>(a, stream);
+    return side == 128 ? launch_plan<TilePlan<2, 4, 2, 1, 64, 2, 2, 2>>(a, stream) : launch_plan<TilePlan<2, 2, 1, 1, 128, 3, 2, 2>>(a, stream);
 }
 
 __global__ __launch_bounds__(256) void gradient_zero_kernel(void *g_w, float *g_bias, size_t words, bool odd, int out)
