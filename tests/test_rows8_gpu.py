@@ -222,3 +222,36 @@ def test_rows_past_32_bits_of_offset():
     want, want_scale = to_8_bits(x.cpu(), 32)
     assert torch.equal(q.cpu(), want) and torch.equal(scale.cpu(), want_scale)
     assert math.isfinite(float(scale.sum()))
+
+
+@pytest.mark.parametrize("name", ["gelu", "silu"])
+def test_values_everywhere(name):
+    """A sweep down to where the values leave the normal numbers and past it, where both functions round to 0."""
+    x = torch.cat((torch.linspace(-15, 15, 400001), torch.linspace(-110, 110, 200001), torch.logspace(-40, 0, 4001), -torch.logspace(-40, 0, 4001)))
+    n = x.numel() // 8
+    x = x[:8 * n].view(8, n)
+    y = filled((8, n), torch.float32)
+    xnor.xnor_activation_q8(x.cuda(), y, None, None, None, None, 8, n, 0, 0, name)
+    a = function(x.double(), name)
+    assert_within(y, a, value_error(x.double(), name) * a.abs() + SMALLEST["f32"], "y")
+
+
+@pytest.mark.parametrize("name", ["gelu", "silu"])
+def test_slopes_everywhere(name):
+    scale = torch.logspace(-12, 0, 1500)[:, None]
+    kept = torch.arange(-127, 128).to(torch.int8).expand(1500, 255).contiguous()
+    g_x = filled((1500, 255), torch.float32)
+    xnor.xnor_activation_backward(kept.cuda(), scale.cuda(), torch.ones((1500, 255), device="cuda"), g_x, 1500, 255, 0, name)
+    values = (kept.float() * scale).double()
+    want, err = gradient_of(values, torch.ones_like(values), name, False)
+    assert_within(g_x, want, err + EPS32 * want.abs() + SMALLEST["f32"], "g_x")
+
+
+@pytest.mark.parametrize("name", ["gelu", "silu"])
+def test_infinities_of_smooth_functions(name):
+    inf, nan = float("inf"), float("nan")
+    x = torch.tensor([[inf, -inf, nan, 3.0e38, -3.0e38, 0.0, -0.0, 1.0e-45]]).cuda()
+    y = filled((1, 8), torch.float32)
+    xnor.xnor_activation_q8(x, y, None, None, None, None, 1, 8, 0, 0, name)
+    y = y.cpu()[0]
+    assert y[0] == inf and y[1] == 0 and y[2].isnan() and y[3] == x[0, 3].cpu() and bool((y[4:7] == 0).all()) and 0 <= float(y[7]) <= 1.5e-45
