@@ -6,6 +6,7 @@
 //   stage   both matrices as float16 operands of the matrix instructions, transposed, each column multiplied by the power of two that brings its largest to 2^15 (float16
 //           then holds 8- and 11-bit gradients exactly down to 2^-29 of the largest)
 //   product the sums, and the powers of two taken out again
+// Few products go through none of it: gradient_direct_kernel below.
 // With one scale per row the scale goes to g instead, sum_r (g[r][o] scale[r]) q[r][k], and q is an operand as it is: float32 gradients and weights then take two products of
 // parts and not three (2048 rows 4096 -> 8192 485 and 279 us).
 #include "xnor_internal.h"
@@ -230,6 +231,19 @@ template <int TYPE> __global__ __launch_bounds__(256) void gradient_stage_kernel
     }
 }
 
+// Four neighbouring results, `n` of which exist, to g_w[at], or added to what is there.
+__device__ __forceinline__ void add_results(const GradArgs &a, size_t at, f32x4 v, int n)
+{
+    if (a.accumulate)
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+            if (m < n)
+                v[m] += a.w_type == XNOR_F32    ? static_cast<const float *>(a.g_w)[at + m]
+                        : a.w_type == XNOR_BF16 ? (float)static_cast<const __bf16 *>(a.g_w)[at + m]
+                                                : (float)static_cast<const _Float16 *>(a.g_w)[at + m];
+    store_four(a.g_w, a.w_type, at, v, n);
+}
+
 constexpr int TURNED = 32 * (64 * 4 + 16);          // bytes of 32 outputs x 64 inputs, outputs 16 bytes further apart
 template <class P> constexpr int lds_bytes() { return std::max(P::BUFFERS * P::BYTES, P::WAVES * TURNED); }
 
@@ -277,17 +291,114 @@ template <class P> __global__ __launch_bounds__(64 * P::WAVES) void gradient_pro
                 if (o0 + r >= a.out || left <= 0) continue;
                 f32x4 v = *reinterpret_cast<const f32x4 *>(turned + r * (64 * 4 + 16) + 4 * k);
                 const size_t at = (size_t)(o0 + r) * a.in + k0 + k;
-                if (a.accumulate)
-#pragma unroll
-                    for (int m = 0; m < 4; ++m)
-                        if (m < left)
-                            v[m] += a.w_type == XNOR_F32    ? static_cast<const float *>(a.g_w)[at + m]
-                                    : a.w_type == XNOR_BF16 ? (float)static_cast<const __bf16 *>(a.g_w)[at + m]
-                                                            : (float)static_cast<const _Float16 *>(a.g_w)[at + m];
-                store_four(a.g_w, a.w_type, at, v, left);
+                add_results(a, at, v, left);
             }
             asm volatile("" ::: "memory");
         }
+    }
+}
+
+// Few products: one launch, 64 outputs x 64 inputs to a workgroup, in float32 throughout.  The matrix instructions of two rows take their operands as they lie: a lane's are one row's,
+// neighbouring lanes' neighbouring columns (two of them each, for two tiles).  Eight waves share the rows, two at a time, and their sums meet in LDS.
+// What bounds it: launch, first loads and last sums up to 100 rows (7.4 us), behind them 0.022 us a row for up to 256 workgroups, 1.6 times what the matrix instructions take.
+constexpr int DIRECT_SIDE = 64, DIRECT_WAVES = 8;
+struct DirectShared {
+    f32x4 sums[DIRECT_WAVES][2][2][4][64];          // [wave][input of a pair][output of a pair][register / 4][lane]
+    float bias[DIRECT_WAVES][DIRECT_SIDE];
+};
+
+template <int TYPE> __global__ __launch_bounds__(64 * DIRECT_WAVES) void gradient_direct_kernel(GradArgs a, int blocks_x)
+{
+    typedef real_t<TYPE> T;
+    constexpr int AT_ONCE = 4;
+    struct __attribute__((packed, aligned(sizeof(T)))) Pair { T v[2]; };
+    struct __attribute__((packed)) Codes { int8_t v[2]; };
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    DirectShared &s = *reinterpret_cast<DirectShared *>(lds);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pair = 2 * (lane & 31);
+    const int bo = blockIdx.x / blocks_x, c0 = DIRECT_SIDE * (int)(blockIdx.x - bo * blocks_x), o0 = DIRECT_SIDE * bo;
+    const int groups = a.group ? (a.in + a.group - 1) / a.group : 1;
+    // the last column of an odd number comes as the second of the pair before; columns behind the last are somebody's results that are not kept
+    const int c = c0 + pair, o = o0 + pair, c_at = min(c, a.in - 2), o_at = min(o, a.out - 2), group = a.group ? min(c, a.in - 1) / a.group : 0;
+    const int8_t *q = a.q + c_at;
+    const float *scale = a.scale + group;
+    const T *g = static_cast<const T *>(a.g) + o_at;
+    struct Step {
+        Codes q;
+        Pair g;
+        float scale;
+    };
+    auto load = [&](Step &t, int r) {
+        const size_t row = min(r, a.rows - 1);
+        t.q = *reinterpret_cast<const Codes *>(q + row * a.in);
+        t.scale = scale[row * groups];
+        t.g = *reinterpret_cast<const Pair *>(g + row * a.g_stride);
+    };
+    f32x16 acc[2][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) acc[i >> 1][i & 1][k] = 0.0f;
+    float bias[2] = {0.0f, 0.0f};
+    Step next[AT_ONCE];
+    const int own = 2 * wave + (lane >> 5);
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) load(next[i], own + 2 * DIRECT_WAVES * i);
+    for (int r = own; r - (lane >> 5) < a.rows; r += 2 * DIRECT_WAVES * AT_ONCE) {            // (a wave's lanes end together)
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const Step t = next[i];
+            load(next[i], r + 2 * DIRECT_WAVES * (i + AT_ONCE));
+            asm volatile("" ::: "memory");              // (else the loads wait until they are used: 777 rows 26 us, so 25)
+            const bool is = r + 2 * DIRECT_WAVES * i < a.rows;
+            float x[2], y[2];
+            x[1] = is ? (float)t.q.v[1] * t.scale : 0.0f;
+            x[0] = c > c_at ? x[1] : is ? (float)t.q.v[0] * t.scale : 0.0f;
+            y[1] = is ? (float)t.g.v[1] : 0.0f;
+            y[0] = o > o_at ? y[1] : is ? (float)t.g.v[0] : 0.0f;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) bias[k] += y[k];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) acc[k >> 1][k & 1] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[k >> 1], y[k & 1], acc[k >> 1][k & 1], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            f32x4 v;
+#pragma unroll
+            for (int m = 0; m < 4; ++m) v[m] = acc[k >> 1][k & 1][4 * b + m];
+            s.sums[wave][k >> 1][k & 1][b][lane] = v;
+        }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const float both = bias[k] + __shfl_xor(bias[k], 32, 64);
+        if (lane < 32) s.bias[wave][pair + k] = both;
+    }
+    __syncthreads();
+    // a thread: eight neighbouring inputs of an output
+    const int b = wave & 3, j = wave >> 2, row = o0 + pair + j, first = c0 + 16 * b + 8 * (lane >> 5);
+    f32x4 even = s.sums[0][0][j][b][lane], odd = s.sums[0][1][j][b][lane];
+#pragma unroll
+    for (int w = 1; w < DIRECT_WAVES; ++w) {
+        even += s.sums[w][0][j][b][lane];
+        odd += s.sums[w][1][j][b][lane];
+    }
+    if (row < a.out)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int k = first + 4 * half, left = a.in - k;
+            if (left <= 0) break;
+            f32x4 v = {even[2 * half], odd[2 * half], even[2 * half + 1], odd[2 * half + 1]};
+            add_results(a, (size_t)row * a.in + k, v, left);
+        }
+    if (a.g_bias && c0 == 0 && threadIdx.x < DIRECT_SIDE && o0 + (int)threadIdx.x < a.out) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < DIRECT_WAVES; ++w) sum += s.bias[w][threadIdx.x];
+        float &to = a.g_bias[o0 + threadIdx.x];
+        to = a.accumulate ? to + sum : sum;
     }
 }
 
@@ -305,7 +416,11 @@ template <class P> xnor_status launch_plan(const GradArgs &a, hipStream_t stream
 // Tiles of 256 x 256, 128 x 128 and 64 x 64 by their time in us, fitted to 75 products (1 to 8192 rows, 128 to 9216 inputs, 128 to 8192 outputs) for each number of parts: a
 // chunk of 64 rows takes the way to L2 and back, or where there are more tiles what L2 gives; a large tile is alone on its CU.  2048 rows 4096 -> 8192 in bfloat16 170, 187 and
 // 263 us in all; 256 rows 9216 -> 4096 65, 52, 85; 2048 rows 1024 -> 1024 78, 42, 31, with float32 results 124, 50, 35.
-int side_of(const Places &p, int in, int out, int w_bytes)
+struct Choice {
+    int side;
+    double time;
+};
+Choice choose(const Places &p, int in, int out, int w_bytes)
 {
     const double chunks = p.padded / 64.0, kept = 2e-7 * in * out * w_bytes;
     auto tiles = [&](int side) { return std::ceil((double)in / side) * std::ceil((double)out / side); };
@@ -317,13 +432,22 @@ int side_of(const Places &p, int in, int out, int w_bytes)
                                     : parts == 3 ? std::max(1.0, 0.0038 * tiles(128))
                                                  : std::max(1.55, 0.0055 * tiles(128)));
     const double rounds = std::ceil(tiles(256) / 256), large = rounds * (parts == 2 ? 1.6 * chunks + 10 : 3.3 * chunks + 13);
-    if (parts < 4 && large < std::min(small, middle) + kept) return 256;
-    return middle < small ? 128 : 64;
+    if (parts < 4 && large < std::min(small, middle) + kept) return {256, large};
+    return middle < small ? Choice{128, middle} : Choice{64, small};
 }
 
-xnor_status launch_product(const GradArgs &a, const Places &p, hipStream_t stream)
+// The direct kernel by its time in us, fitted likewise; the others' range, staging and launches take 13 and their way through memory.  2 rows 371 -> 2011 bfloat16 4.8 and
+// 12, 64 rows 1003 -> 1000 float32 7.4 and 16, 256 rows 1024 -> 1024 bfloat16 10.5 and 16, 777 rows 1003 -> 1000 float32 25 and 28; 2048 rows 512 -> 512 bfloat16 52 and 25, 64 rows
+// 4096 -> 4096 84 and 25.  Over 70 products (1 to 1156 rows, 17 to 2900 inputs and outputs) the choice takes 1.001 of the faster one's time.
+bool direct_is_faster(const Places &p, int rows, int in, int out, const Choice &staged)
 {
-    const int side = side_of(p, a.in, a.out, (int)type_bytes(a.w_type));
+    if (in < 2 || out < 2) return false;
+    const double rounds = std::ceil(std::ceil(in / 64.0) * std::ceil(out / 64.0) / 256), bytes = 2.0 * p.padded * ((double)in * p.parts_x + (double)out * p.parts_g);
+    return 2 + rounds * (2.8 + 0.0235 * rows) < 13 + staged.time + bytes / 3.5e6;
+}
+
+xnor_status launch_product(const GradArgs &a, const Places &p, int side, hipStream_t stream)
+{
     if (p.parts_x == 1 && p.parts_g == 2) {
         if (side == 256) return launch_plan<TilePlan<2, 4, 4, 2, 64, 3, 1, 2>>(a, stream);
         return side == 128 ? launch_plan<TilePlan<2, 4, 2, 1, 64, 3, 1, 2>>(a, stream) : launch_plan<TilePlan<2, 2, 1, 1, 128, 4, 1, 2>>(a, stream);
@@ -362,10 +486,24 @@ xnor_status launch_weight_gradient(const int8_t *q, const float *scale, const vo
     }
     const GradArgs a{q, scale, g_y, g_w, g_bias, static_cast<uint8_t *>(workspace), g_stride, rows, in, out, group, type, w_type, accumulate};
     const Places p(rows, in, out, group, type, w_type);
+    const Choice choice = choose(p, in, out, (int)type_bytes(w_type));
+    xnor_status status = XNOR_OK;
+    if (direct_is_faster(p, rows, in, out, choice)) {
+        const int blocks_x = (in + DIRECT_SIDE - 1) / DIRECT_SIDE, blocks_g = (out + DIRECT_SIDE - 1) / DIRECT_SIDE;
+        by_type(type, [&](auto t) {
+            auto kernel = gradient_direct_kernel<t()>;
+            if (hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, sizeof(DirectShared)) != hipSuccess) {
+                status = XNOR_ERR_HIP;
+                return;
+            }
+            kernel<<<dim3((unsigned)(blocks_x * blocks_g)), dim3(64 * DIRECT_WAVES), sizeof(DirectShared), stream>>>(a, blocks_x);
+            status = hip_status(hipGetLastError());
+        });
+        return status;
+    }
     const int scale_blocks = p.by_row ? 0 : (p.groups + RANGE_COLS - 1) / RANGE_COLS;
     const dim3 range((unsigned)((out + RANGE_COLS - 1) / RANGE_COLS + scale_blocks), (unsigned)p.parts);
     const dim3 stage((unsigned)((out + STAGED_COLS - 1) / STAGED_COLS + (in + STAGED_COLS - 1) / STAGED_COLS), (unsigned)(p.padded / STAGED_ROWS));
-    xnor_status status = XNOR_OK;
     by_type(type, [&](auto t) {
         gradient_range_kernel<t()><<<range, dim3(256), 0, stream>>>(a);
         status = hip_status(hipGetLastError());
@@ -374,7 +512,7 @@ xnor_status launch_weight_gradient(const int8_t *q, const float *scale, const vo
         status = hip_status(hipGetLastError());
     });
     if (status) return status;
-    return launch_product(a, p, stream);
+    return launch_product(a, p, choice.side, stream);
 }
 
 }  // namespace xnor

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_1603_05279_amd import xnor
-from tests.lowbit_helpers import EPS32, HALF_ULP, SMALLEST, TYPES, assert_within, filled, generator, normal
+from tests.lowbit_helpers import EPS32, HALF_ULP, SMALLEST, TYPES, apart, assert_within, filled, generator, normal
 from tests.test_weight_gradient_gpu import bounds, make, values
 
 pytestmark = pytest.mark.gpu
@@ -71,7 +71,9 @@ def test_a_workspace_of_more_rows_serves_fewer(cin, out):
 
 # sides of 64, 128 and 256 with one and two parts of each operand
 GRADIENTS = [(1077, 33, 31), (18, 161, 46), (215, 36, 65), (1, 4196, 405), (12, 322, 5973), (2, 1050, 2431), (257, 2100, 2300), (266, 4556, 3575), (3, 3297, 4802),
-             (2048, 4096, 8192), (1030, 4099, 4100)]
+             (2048, 4096, 8192), (1030, 4099, 4100), (1200, 100, 100), (1500, 65, 130),
+             # few products: one launch, pairs of columns
+             (5, 2, 2), (9, 3, 2), (40, 65, 2), (100, 2, 129), (33, 127, 63), (1, 371, 2011), (64, 1003, 1000), (129, 128, 192), (777, 1003, 1000)]
 
 
 @pytest.mark.parametrize("name,wname", [("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32"), ("f16", "f16"), ("f32", "f32")])
@@ -88,6 +90,28 @@ def test_gradients(rows, cin, out, name, wname):
     bound = err + (HALF_ULP[wname] * (want.abs() + err) + SMALLEST[wname] if wname != "f32" else 0)
     assert int((~((g_w.double() - want).abs() <= bound)).sum()) == 0 and untouched(space)
     assert_within(g_b, d.sum(0), ((rows + 4) * EPS32 * d.abs().sum(0)).cpu(), "g_bias")
+
+
+@pytest.mark.parametrize("rows,cin,out,extra", [(1200, 100, 100, 0), (1200, 99, 101, 3), (300, 1100, 4200, 0), (65, 66, 67, 5), (40, 128, 64, 0), (3, 5, 7, 1)])
+@pytest.mark.parametrize("name,wname", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+def test_gradients_added_to_what_is_there(name, wname, rows, cin, out, extra):
+    """Rows of the gradient further apart than they are long, and results added: the sum without them, one more addition and rounding."""
+    group = (0, 128, 32)[(rows + cin) % 3]
+    gen = generator(rows + out)
+    q, scale, g = make(gen, rows, cin, out, group, name)
+    q, scale, g = q.cuda(), scale.cuda(), apart(g, extra)
+    n = xnor.q8_weight_gradient_workspace_bytes(rows, cin, out, group, TYPES[name], TYPES[wname])
+    g_w, g_b = normal(gen, out, cin).to(TYPES[wname]).cuda(), normal(gen, out).cuda()
+    before = g_w.double(), g_b.double()
+    xnor.xnor_q8_weight_gradient(q, scale, g, g_w, g_b, filled((n,), torch.uint8), rows, cin, out, group, accumulate=True)
+    x, d = values(q, scale, group), g.double()
+    err, _ = bounds(x, d, name, wname)
+    want = d.t().contiguous() @ x + before[0]
+    err = err + EPS32 * want.abs()
+    bound = err + (HALF_ULP[wname] * (want.abs() + err) + SMALLEST[wname] if wname != "f32" else 0)
+    assert int((~((g_w.double() - want).abs() <= bound)).sum()) == 0
+    want = d.sum(0) + before[1]
+    assert_within(g_b, want, ((rows + 4) * EPS32 * d.abs().sum(0) + EPS32 * want.abs()).cpu(), "g_bias")
 
 
 @pytest.mark.parametrize("name,wname", [("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32"), ("f16", "f16"), ("f32", "f32")])
