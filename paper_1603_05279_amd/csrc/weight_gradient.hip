@@ -300,7 +300,8 @@ template <class P> __global__ __launch_bounds__(64 * P::WAVES) void gradient_pro
 
 // Few products: one launch, 64 outputs x 64 inputs to a workgroup, in float32 throughout.  The matrix instructions of two rows take their operands as they lie: a lane's are one row's,
 // neighbouring lanes' neighbouring columns (two of them each, for two tiles).  Eight waves share the rows, two at a time, and their sums meet in LDS.
-// What bounds it: launch, first loads and last sums up to 100 rows (7.4 us), behind them 0.022 us a row for up to 256 workgroups, 1.6 times what the matrix instructions take.
+// What bounds it: launch, first loads and last sums up to 100 rows (7.4 us), behind them 0.022 us a row for up to 256 workgroups, 1.6 times what the matrix instructions take
+// at 2.4 GHz (addresses by steps in place of products, more rows ahead: no change).
 constexpr int DIRECT_SIDE = 64, DIRECT_WAVES = 8;
 struct DirectShared {
     f32x4 sums[DIRECT_WAVES][2][2][4][64];          // [wave][input of a pair][output of a pair][register / 4][lane]
