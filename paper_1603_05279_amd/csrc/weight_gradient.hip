@@ -212,7 +212,7 @@ template <int TYPE> __global__ __launch_bounds__(256) void gradient_stage_kernel
     // eight lanes write the 64 rows of a column
     const int parts = is_g ? p.parts_g : p.parts_x;
     uint8_t *to = a.work + (is_g ? p.g_at : p.x_at);
-#pragma unroll
+#pragma unroll 1
     for (int i = 0; i < STAGED_COLS * STAGED_ROWS / 8 / 256; ++i) {
         const int unit = tid + 256 * i, col = unit >> 3, r = 8 * (unit & 7);
         if (c0 + col >= cols) break;
