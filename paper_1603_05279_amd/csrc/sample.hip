@@ -48,13 +48,16 @@ struct SampleArgs {
 
 // A row's distances and weights.
 struct Weigh {
-    float half_top, bin_factor;
+    float part, part_top, bin_factor;
     double top, factor, whole;
     const double *table;            // 2^(i / 256)
     __device__ __forceinline__ Weigh(float largest, float T, int bits, const double *powers)
     {
-        half_top = 0.5f * largest;
-        bin_factor = fminf(2.0f * PER_E / T, 0x1.fffffep127f);
+        // temperatures near the ends of float32 weigh logits as close together, if these are small themselves (others are 2^75 temperatures apart, or the same)
+        const bool close = T < 0x1p-100f && __builtin_fabsf(largest) < 1.0f;
+        part = close ? 0x1p60f : 0.5f;
+        part_top = part * largest;
+        bin_factor = fminf(PER_E / (part * T), 0x1.fffffep127f);
         top = largest;
         factor = PER_OCTAVE * 0x1.71547652b82fep+0 / (double)T;                // log2 e
         whole = 0x1.8p52 + PER_OCTAVE * bits;
@@ -62,7 +65,7 @@ struct Weigh {
     }
     // in bins, as a real number: in 32 bits, where it never falls as the logit falls (both roundings keep the order), and that is all a bin has to do.  (From the halves: the
     // distance itself may be out of range.)
-    __device__ __forceinline__ float bins(float l) const { return __builtin_fmaf(l, -0.5f, half_top) * bin_factor; }
+    __device__ __forceinline__ float bins(float l) const { return __builtin_fmaf(l, -part, part_top) * bin_factor; }
     __device__ __forceinline__ static int bin(float b) { return (int)fminf(b, BINS - 1); }
     // in 256ths of a factor of two
     __device__ __forceinline__ double distance(float l) const { return (top - (double)l) * factor; }
