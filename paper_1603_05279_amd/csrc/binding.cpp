@@ -7,6 +7,7 @@
 // been told; sizes are the caller's, as in the C ABI.  The library's entry points are looked up in the file that xnor.py
 // names (bind), so that another build of it can be called.
 #include <c10/core/impl/DeviceGuardImplInterface.h>
+#include <torch/csrc/Device.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <dlfcn.h>
@@ -129,11 +130,24 @@ int64_t groups(int64_t cols, int64_t group) { return group > 0 ? (cols + group -
 XNOR_QUERIES(XNOR_QUERY_POINTER)
 void *bytes(PyObject *o, size_t count) { return dense(o, c10::ScalarType::Byte, (int64_t)count); }
 
-// The tensors among a call's arguments (the stream, last, is None or not) have to be on one device, the current one where no stream is given: a kernel would
+// The device of a stream object, -1 where it does not say (a handle by itself).
+int device_of(PyObject *stream)
+{
+    PyObject *device = PyObject_GetAttrString(stream, "device");
+    if (!device) {
+        if (!PyErr_ExceptionMatches(PyExc_AttributeError)) throw PythonError{};
+        PyErr_Clear();
+        return -1;
+    }
+    const int index = THPDevice_Check(device) ? (int)reinterpret_cast<THPDevice *>(device)->device.index() : -1;
+    Py_DECREF(device);
+    return index;
+}
+// The tensors among a call's arguments have to be on one device, that of the stream (the last argument) or, where none is given, the current one: a kernel would
 // read another's memory, or run on a device that does not hold its tensors.  Returns `value`, so that a call's last number can stand for the check.
 int on_one_device(PyObject *const *a, int n, int value)
 {
-    int device = a[n - 1] == Py_None ? (int)c10::impl::getDeviceGuardImpl(c10::DeviceType::CUDA)->getDevice().index() : -1;
+    int device = a[n - 1] == Py_None ? (int)c10::impl::getDeviceGuardImpl(c10::DeviceType::CUDA)->getDevice().index() : device_of(a[n - 1]);
     for (int i = 0; i < n - 1; ++i) {
         if (!THPVariable_Check(a[i])) continue;
         const int here = (int)THPVariable_Unpack(a[i]).get_device();
