@@ -926,7 +926,7 @@ struct Part {
     uint32_t listed, seen;          // seen, plan: of the first part only, for the row
     Plan plan;
 };
-constexpr int PART_FRACTION = 12, MEAN_BITS = 19, PART_TOKENS = 8184, MOST_PARTS = 32, MOST_WORKGROUPS = 256;
+constexpr int PART_FRACTION = 12, MEAN_BITS = 19, PART_TOKENS = 8184, MOST_PARTS = 64, MOST_WORKGROUPS = 256;
 static_assert(PART_TOKENS < 1 << (32 - MEAN_BITS) && (uint64_t)MOST_PARTS * PART_TOKENS << PART_FRACTION < 1ull << 32);
 
 template <int TYPE> __device__ __forceinline__ Slice<TYPE> slice_of(const SampleArgs &a, size_t r, int part)
@@ -1060,7 +1060,8 @@ template <int TYPE> __global__ __launch_bounds__(1024) void sample_draw_kernel(S
 
 // Parts of a row (1: a row per workgroup): of 8000 tokens or so, for few rows of long vocabularies.  A workgroup takes 0.4 us for 1000 tokens that are all weighed, its parts
 // 4 launches.  In one and in parts, with top_p: 1 x 128000 bfloat16 66 and 32 us, 16 x 128000 74 and 45, 1 x 41000 30 and 28, 24 x 64000 42 and 37, 1 x 32000 26 and 28, 32 x 50000
-// 35 and 37, 64 x 64000 46 and 66.  With top_k few are weighed: 40 and 43 (1 x 128000), 29 and 37, 21 and 29.
+// 35 and 37, 64 x 64000 46 and 66, 1 x 262144 129 and 42, 4 x 523776 250 and 59.  With top_k few are weighed: 40 and 43 (1 x 128000), 29 and 37, 21 and 29.  (No more parts
+// than a wave has lanes, which join what they hand on.)
 int row_parts(int rows, int vocab, bool top_k)
 {
     const int parts = (vocab + PART_TOKENS - 1) / PART_TOKENS;
