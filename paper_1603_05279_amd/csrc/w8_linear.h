@@ -12,9 +12,7 @@ struct W8Args {
     int rows, in, out, type;
 };
 
-constexpr int W8_LARGE = 256, W8_SMALL = 128;           // sides of the tiles of w8_tiles.hip
-
-// side: one of those; shares (of the inputs, W8_SMALL only): that many times rows x out sums of 32 bits, in whole tiles, in a.work
+// side: W8_LARGE or W8_SMALL; shares (of the inputs, W8_SMALL only): that many times rows x out sums of 32 bits, in whole tiles, in a.work
 xnor_status launch_w8_tiles(const W8Args &a, int side, int shares, hipStream_t stream);
 
 }  // namespace xnor

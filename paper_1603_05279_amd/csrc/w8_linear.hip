@@ -2,6 +2,7 @@
 #include "xnor_internal.h"
 #include "lowbit.h"
 #include "w8_form.h"
+#include "w8_choice.h"
 #include "w8_linear.h"
 #include <algorithm>
 #include <cmath>
@@ -94,80 +95,17 @@ xnor_status launch_rows(W8Args a, int tiles, hipStream_t stream)
     return XNOR_OK;
 }
 
-// Which kernel takes a product: the shortest of their times in us, fitted to 150 products (inputs 256 to 9216, outputs 256 to 8192, 1 to 2048 rows, half of them no multiple of
-// anything).
-struct Choice {
-    int tiles, side, shares;        // w8_rows_kernel's row tiles, or the side of w8_tiles.hip's tiles and the shares of the inputs
-    double time;
-};
-
-double blocks(int n, int side) { return std::ceil((double)n / side); }
-
-// w8_rows_kernel reads every weight once per 16, 32 or 64 rows and splits the inputs over its waves.  One, two and four tiles: 16 rows 9216 -> 4096 10.6, 11.5, 13.6; 32 rows
-// 4096 -> 4096 10.0, 8.1, 9.2; 64 rows 17, 13.5, 11.7 (128 x 128 in four shares 15).  Rows that start between words of 32 bits: 15 rows 6086 -> 7076 31 (in shares 24).
-Choice by_rows(int rows, int in, int out)
-{
-    const double turns = std::ceil(std::ceil(in / 128.0) / 8);
-    Choice best{0, 0, 1, 0.0};
-    for (int tiles : {1, 2, 4}) {
-        const double n = blocks(out, 16) * blocks(rows, 16 * tiles) / 256;
-        const double time = 4.3 + (tiles == 1 ? 0.85 : tiles == 2 ? 1.2 : 2.05) * (in % 4 ? 2.4 : 1.0) * turns * std::max(n, 0.7);
-        if (best.tiles == 0 || time < best.time) best = {tiles, 0, 1, time};
-    }
-    return best;
-}
-// Tiles of 128 x 128: what a CU gets out of L2 bounds a chunk, 0.65 us for 256 workgroups (12 TB/s), and its way there and back where there are fewer.  In shares of the inputs
-// where that fills the chip, which costs another launch and the sums' way through memory.  256 rows 9216 -> 4096 in 1, 2, 3, 4 and 6 shares 39, 26, 24, 26, 28; 512 rows
-// 4096 -> 4096 in 1 and 2 21, 25.
-Choice by_small_tiles(int row_blocks, int in, int out)
-{
-    const double chunks = std::ceil(in / 128.0), tiles = (double)row_blocks * blocks(out, W8_SMALL);
-    Choice best{0, W8_SMALL, 0, 0.0};
-    for (int shares : {1, 2, 3, 4, 6, 8}) {
-        const double n = tiles * shares / 256;
-        if (shares > 1 && (n > 2 || chunks < 2 * shares)) break;
-        const double chunk = in % 16 == 0 ? std::max(0.48, 0.65 * n) : in % 4 == 0 ? std::max(0.85, 0.85 * n) : std::max(1.25, 0.95 * n);
-        const double time = 4.0 + chunk * std::ceil(chunks / shares) + (shares > 1 ? 2.5 + 0.026 * tiles * shares : 0.0) + 0.002 * tiles;
-        if (best.shares == 0 || time < best.time) best = {0, W8_SMALL, shares, time};
-    }
-    return best;
-}
-// Tiles of 256 x 256 take half as much out of L2 per result, one workgroup to a CU.  2048 rows 4096 -> 8192 83 us, in tiles of 128 x 128 91; 4096 rows 158, 175; 1024 rows 70, 45.
-Choice by_large_tiles(int rows, int in, int out)
-{
-    const double tiles = blocks(rows, W8_LARGE) * blocks(out, W8_LARGE), rounds = std::ceil(tiles / 256);
-    return {0, W8_LARGE, 1, 12 + (tiles <= 128 ? 0.85 : 1.06) * std::ceil(in / 64.0) * rounds * (in % 4 ? 1.5 : in % 16 ? 1.3 : 1.0) + 0.012 * tiles};
-}
-Choice choose(int rows, int in, int out)
-{
-    Choice best = by_rows(rows, in, out);
-    for (const Choice &c : {by_small_tiles((int)blocks(rows, W8_SMALL), in, out), by_large_tiles(rows, in, out)})
-        if (c.time < best.time) best = c;
-    return best;
-}
-size_t share_bytes(int row_blocks, int in, int out)
-{
-    const int shares = by_small_tiles(row_blocks, in, out).shares;
-    return shares > 1 ? (size_t)shares * row_blocks * (size_t)blocks(out, W8_SMALL) * W8_SMALL * W8_SMALL * 4 : 0;
-}
-
 }  // namespace
 
-bool w8_linear_needs(int rows, int in, int out) { return choose(rows, in, out).shares > 1; }
+bool w8_linear_needs(int rows, int in, int out) { return w8_choice(rows, in, out).shares > 1; }
 
-// (the most of any number of rows up to this one: more than 512 tiles are not shared)
-size_t w8_linear_workspace_bytes(int rows, int in, int out)
-{
-    size_t most = 0;
-    for (int b = 1; b <= (int)blocks(rows, W8_SMALL) && b * blocks(out, W8_SMALL) <= 512; ++b) most = std::max(most, share_bytes(b, in, out));
-    return most;
-}
+size_t w8_linear_workspace_bytes(int rows, int in, int out) { return w8_share_bytes(rows, in, out); }
 
 xnor_status launch_w8_linear(const int8_t *q, const float *x_scale, const int8_t *w, const float *w_scale, const float *bias, void *y, void *workspace, int rows,
                              int in, int out, int type, hipStream_t stream)
 {
     const W8Args a{q, w, x_scale, w_scale, bias, y, workspace, rows, in, out, type};
-    const Choice c = choose(rows, in, out);
+    const W8Choice c = w8_choice(rows, in, out);
     return c.tiles ? launch_rows(a, c.tiles, stream) : launch_w8_tiles(a, c.side, c.shares, stream);
 }
 

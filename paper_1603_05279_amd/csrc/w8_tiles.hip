@@ -2,6 +2,7 @@
 #include "xnor_internal.h"
 #include "lowbit.h"
 #include "tiles.h"
+#include "w8_choice.h"
 #include "w8_linear.h"
 #include <algorithm>
 
@@ -147,9 +148,7 @@ xnor_status launch_w8_tiles(const W8Args &a, int side, int shares, hipStream_t s
 {
     const bool aligned = a.in % 16 == 0;
     if (side == W8_LARGE) return aligned ? launch<Large, true, false>(a, 1, stream) : launch<Large, false, false>(a, 1, stream);
-    const long long count = (long long)((a.rows + Small::B - 1) / Small::B) * ((a.out + Small::A - 1) / Small::A) * shares;
-    // (each alone on its CU: 256 x 4096 -> 4096 20 us, with two chunks in LDS 23; from 256 workgroups on two of them share a CU and its loads better, 512 x 4096 -> 8192 27, 29)
-    if (aligned && count <= 192) return shares > 1 ? launch<Deep, true, true>(a, shares, stream) : launch<Deep, true, false>(a, 1, stream);
+    if (w8_alone(a.rows, a.in, a.out, shares)) return shares > 1 ? launch<Deep, true, true>(a, shares, stream) : launch<Deep, true, false>(a, 1, stream);
     if (shares > 1) return aligned ? launch<Small, true, true>(a, shares, stream) : launch<Small, false, true>(a, shares, stream);
     return aligned ? launch<Small, true, false>(a, 1, stream) : launch<Small, false, false>(a, 1, stream);
 }

@@ -3,17 +3,14 @@
 //     g_w[o][k] = sum_r g[r][o] x[r][k],    x = q * scale
 // is a product of two matrices that both run along the rows, which neither stores next to each other.  Three launches:
 //   range   the largest magnitude of every column of g (and its sum, the bias' gradient) and of the scales, in up to eight parts of the rows
-//   stage   both matrices as float16 operands of the matrix instructions, transposed, each column multiplied by the power of two that brings its largest to 2^15 (float16
-//           then holds 8- and 11-bit gradients exactly down to 2^-29 of the largest)
+//   stage   both matrices as float16 operands of the matrix instructions, transposed, each column multiplied by the power of two that brings its largest to between 2^14 and 2^15
+//           (float16 then holds 8- and 11-bit gradients exactly down to 2^-28 of the largest, and less to 2^-39 of it)
 //   product the sums, and the powers of two taken out again
 // Few products go through none of it: gradient_direct_kernel below.
-// A factor that is more than one float16 holds, q * scale or a float32 gradient (with scales of rows the gradient times the scale), is two of them, 22 bits.  For bfloat16 results
-// q * scale and a 16-bit gradient's product with its scale are one, 11 bits, off by 2^-12 of themselves at most: a sixteenth of the half step top / 254 that the codes were
-// rounded by, an eighth of those of a bfloat16 gradient and of the result (a float16 gradient's own).  2048 rows 4096 -> 8192 in groups, bfloat16 throughout, 164 us, with two
-// parts 262; from float32 gradients, which carry no such rounding and keep their bits, 277 (cut to 11 bits 174).
 // With one scale per row the scale goes to g instead, sum_r (g[r][o] scale[r]) q[r][k], and q is an operand as it is: float32 gradients and weights then take two products of
 // parts and not three (2048 rows 4096 -> 8192 485 and 279 us).
 #include "xnor_internal.h"
+#include "gradient_choice.h"
 #include "lowbit.h"
 #include "tiles.h"
 #include <algorithm>
@@ -23,23 +20,18 @@ namespace xnor {
 
 namespace {
 
-constexpr int STAGED_ROWS = 64, STAGED_COLS = 128;      // of a workgroup of the staging launch
+constexpr int STAGED_COLS = 128;        // of a workgroup of the staging launch
 constexpr int RANGE_COLS = 128, RANGE_PARTS = 8;        // of a workgroup of the first launch; of the rows, at most
 
 // Where the launches keep what they hand on:
 //   x, g     float16 [column][part][row], rows behind the last up to a whole 64 are 0
 //   top, sum [part of the rows][columns]: largest magnitudes of g and of the scales, sums of g
 //   e        exponents of the columns of g and of the groups
-struct Places {
-    int padded, parts_x, parts_g, groups, parts, columns;       // padded: rows
-    bool by_row;                                                // the scales are the rows'
+struct Places : GradientParts {
+    int groups, parts, columns;
     size_t x_at, g_at, top_at, sum_at, e_at, total;
-    __host__ __device__ Places(int rows, int in, int out, int group, int type, int w_type)
+    __host__ __device__ Places(int rows, int in, int out, int group, int type, int w_type) : GradientParts(rows, group, type, w_type)
     {
-        padded = (rows + STAGED_ROWS - 1) / STAGED_ROWS * STAGED_ROWS;
-        by_row = group == 0;
-        parts_x = w_type == XNOR_BF16 || by_row ? 1 : 2;
-        parts_g = type == XNOR_F32 || (by_row && w_type != XNOR_BF16) ? 2 : 1;
         groups = group ? (in + group - 1) / group : 1;
         columns = (out + 3) / 4 * 4 + (groups + 3) / 4 * 4;     // (g's first, the groups from `groups_at` on)
         parts = (rows + 127) / 128 < RANGE_PARTS ? (rows + 127) / 128 : RANGE_PARTS;
@@ -306,7 +298,7 @@ template <class P> __global__ __launch_bounds__(64 * P::WAVES) void gradient_pro
 // neighbouring lanes' neighbouring columns (two of them each, for two tiles).  Eight waves share the rows, two at a time, and their sums meet in LDS.
 // What bounds it: launch, first loads and last sums up to 100 rows (7.4 us), behind them 0.022 us a row for up to 256 workgroups, 1.6 times what the matrix instructions take
 // at 2.4 GHz (addresses by steps in place of products, more rows ahead: no change).
-constexpr int DIRECT_SIDE = 64, DIRECT_WAVES = 8;
+constexpr int DIRECT_WAVES = 8;
 struct DirectShared {
     f32x4 sums[DIRECT_WAVES][2][2][4][64];          // [wave][input of a pair][output of a pair][register / 4][lane]
     float bias[DIRECT_WAVES][DIRECT_SIDE];
@@ -436,39 +428,6 @@ template <class P> xnor_status launch_plan(const GradArgs &a, hipStream_t stream
     return hip_status(hipGetLastError());
 }
 
-// Tiles of 256 x 256, 128 x 128 and 64 x 64 by their time in us, fitted to 75 products (1 to 8192 rows, 128 to 9216 inputs, 128 to 8192 outputs) for each number of parts: a
-// chunk of 64 rows takes the way to L2 and back, or where there are more tiles what L2 gives; a large tile is alone on its CU.  2048 rows 4096 -> 8192 in bfloat16 170, 187 and
-// 263 us in all; 256 rows 9216 -> 4096 65, 52, 85; 2048 rows 1024 -> 1024 78, 42, 31, with float32 results 124, 50, 35.
-struct Choice {
-    int side;
-    double time;
-};
-Choice choose(const Places &p, int in, int out, int w_bytes)
-{
-    const double chunks = p.padded / 64.0, kept = 2e-7 * in * out * w_bytes;
-    auto tiles = [&](int side) { return std::ceil((double)in / side) * std::ceil((double)out / side); };
-    const int parts = p.parts_x + p.parts_g;
-    const double small = chunks * (parts == 2   ? std::max(0.33, 0.00131 * tiles(64))
-                                   : parts == 3 ? std::max(0.5, 0.0018 * tiles(64))
-                                                : std::max(0.65, 0.0019 * tiles(64)));
-    const double middle = chunks * (parts == 2   ? std::max(0.6, 0.0023 * tiles(128))
-                                    : parts == 3 ? std::max(1.0, 0.0038 * tiles(128))
-                                                 : std::max(1.55, 0.0055 * tiles(128)));
-    const double rounds = std::ceil(tiles(256) / 256), large = rounds * (parts == 2 ? 1.6 * chunks + 10 : 3.3 * chunks + 13);
-    if (parts < 4 && large < std::min(small, middle) + kept) return {256, large};
-    return middle < small ? Choice{128, middle} : Choice{64, small};
-}
-
-// The direct kernel by its time in us, fitted likewise; the others' range, staging and launches take 13 and their way through memory.  2 rows 371 -> 2011 bfloat16 4.8 and
-// 12, 64 rows 1003 -> 1000 float32 7.4 and 16, 256 rows 1024 -> 1024 bfloat16 10.5 and 16, 777 rows 1003 -> 1000 float32 25 and 28; 2048 rows 512 -> 512 bfloat16 52 and 25, 64 rows
-// 4096 -> 4096 84 and 25.  Over 70 products (1 to 1156 rows, 17 to 2900 inputs and outputs) the choice takes 1.001 of the faster one's time.
-bool direct_is_faster(const Places &p, int rows, int in, int out, const Choice &staged)
-{
-    if (in < 2 || out < 2) return false;
-    const double rounds = std::ceil(std::ceil(in / 64.0) * std::ceil(out / 64.0) / 256), bytes = 2.0 * p.padded * ((double)in * p.parts_x + (double)out * p.parts_g);
-    return 2 + rounds * (2.8 + 0.0235 * rows) < 13 + staged.time + bytes / 3.5e6;
-}
-
 xnor_status launch_product(const GradArgs &a, const Places &p, int side, hipStream_t stream)
 {
     if (p.parts_x == 1 && p.parts_g == 2) {
@@ -509,9 +468,9 @@ xnor_status launch_weight_gradient(const int8_t *q, const float *scale, const vo
     }
     const GradArgs a{q, scale, g_y, g_w, g_bias, static_cast<uint8_t *>(workspace), g_stride, rows, in, out, group, type, w_type, accumulate};
     const Places p(rows, in, out, group, type, w_type);
-    const Choice choice = choose(p, in, out, (int)type_bytes(w_type));
+    const GradientChoice choice = gradient_choice(p, rows, in, out, (int)type_bytes(w_type));
     xnor_status status = XNOR_OK;
-    if (direct_is_faster(p, rows, in, out, choice)) {
+    if (choice.direct) {
         const int blocks_x = (in + DIRECT_SIDE - 1) / DIRECT_SIDE, blocks_g = (out + DIRECT_SIDE - 1) / DIRECT_SIDE;
         by_type(type, [&](auto t) {
             auto kernel = gradient_direct_kernel<t()>;
