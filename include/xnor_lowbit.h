@@ -219,8 +219,8 @@ XNOR_API int xnor_activation_backward(const int8_t *kept, const float *kept_scal
  * Few products run in float32 throughout; the others on the 16-bit matrix instructions with float32 sums.  There a row's value q * scale and a float32
  * gradient enter as two 11-bit floats (22 bits), 16-bit gradients as they are; with group 0 q enters as it is and g_y * scale as two such floats.  For XNOR_BF16 results one takes the
  * place of two, but for float32 gradients (and their products with the scales of rows).  Both sides are first
- * multiplied by powers of two that bring each column's largest (of a group: what its largest scale makes of a code of 127) to 2^15, and what is 2^-29 of that or less keeps its value to
- * 2^-40 of it.  A scale may be any finite number: only its products with gradients have to be within float32's range.  A row of g_w whose gradients hold an
+ * multiplied by powers of two that bring each column's largest (of a group: what its largest scale makes of a code of 128) to between 2^14 and 2^15; what is then below 2^-14 keeps its
+ * value to 2^-25, at most 2^-39 of that largest.  A scale may be any finite number: only its products with gradients have to be within float32's range.  A row of g_w whose gradients hold an
  * infinity or a NaN is not finite; neither are a group's columns with a scale that is not.  The order of the sums follows from the sizes alone.
  * With rows = 0 the results are zeros (accumulate: left as they are).  in * out <= 2^35, XNOR_ERR_SHAPE otherwise.
  */
