@@ -173,7 +173,7 @@ XNOR_API int xnor_q8_rows(const void *x, int64_t x_stride, int8_t *q, float *sca
  *   bias     in   (nullable) float32 [out]
  *   y        out  `type` [rows][out]
  *   workspace     xnor_w8_linear_workspace_bytes(rows, in, out) bytes, may be NULL where that is 0
- * in <= 131071 (sums within 32 bits), XNOR_ERR_UNSUPPORTED otherwise.
+ * in <= 131071 (sums within 32 bits), XNOR_ERR_UNSUPPORTED otherwise.  From 2^23 tiles of 256 x 256 results on (2^39 of them, more than the memory holds): XNOR_ERR_SHAPE.
  */
 XNOR_API size_t xnor_w8_linear_workspace_bytes(int rows, int in, int out);
 XNOR_API int xnor_w8_linear(const int8_t *q, const float *x_scale, const int8_t *w, const float *w_scale, const float *bias, void *y, void *workspace,
@@ -190,7 +190,7 @@ XNOR_API int xnor_w8_linear(const int8_t *q, const float *x_scale, const int8_t 
  *   kept, kept_scale
  *               out  (nullable) int8 [rows][cols or 2 cols], float32 [rows][groups of kept_group of those columns, or 1]: what xnor_q8_rows makes of x
  *   group, kept_group   0, 32, 64 or 128 columns
- * One of y, q and kept is required.  cols <= 2^23.
+ * One of y, q and kept is required.  cols <= 2^23; in the backward pass rows * ceil(cols / 2048) < 2^24 - 1, XNOR_ERR_SHAPE otherwise.
  *
  * Backward pass, from what was kept: with x^ = kept * kept_scale
  *     g_x = g_y f'(x^),  f'(0) = 0 for XNOR_RELU;     gated: g_x[:, :cols] = g_y x^[:, cols:] f'(x^[:, :cols]),  g_x[:, cols:] = g_y f(x^[:, :cols])

@@ -7,6 +7,7 @@
 namespace xnor {
 
 constexpr int W8_LARGE = 256, W8_SMALL = 128;           // sides of the tiles of w8_tiles.hip
+constexpr long long W8_MOST_TILES = 0xffffff00LL / 512;    // of a launch, whose threads are counted in 32 bits
 
 // The shortest of their times in us, fitted to 150 products (inputs 256 to 9216, outputs 256 to 8192, 1 to 2048 rows, half of them no multiple of
 // anything).
@@ -55,8 +56,9 @@ inline W8Choice w8_by_large_tiles(int rows, int in, int out)
 inline W8Choice w8_choice(int rows, int in, int out)
 {
     W8Choice best = w8_by_rows(rows, in, out);
-    for (const W8Choice &c : {w8_by_small_tiles((int)w8_blocks(rows, W8_SMALL), in, out), w8_by_large_tiles(rows, in, out)})
-        if (c.time < best.time) best = c;
+    const W8Choice small = w8_by_small_tiles((int)w8_blocks(rows, W8_SMALL), in, out), large = w8_by_large_tiles(rows, in, out);
+    if (small.time < best.time && w8_blocks(rows, W8_SMALL) * w8_blocks(out, W8_SMALL) <= W8_MOST_TILES) best = small;
+    if (large.time < best.time) best = large;
     return best;
 }
 // Bytes of the shares' sums: the most of any number of rows up to this one.  (More than 256 tiles are not shared.)

@@ -126,7 +126,8 @@ template <class P, bool ALIGNED, bool SHARES> xnor_status launch(const W8Args &a
     constexpr unsigned lds = lds_bytes<P, SHARES>();
     const int row_blocks = (a.rows + P::B - 1) / P::B, out_blocks = (a.out + P::A - 1) / P::A;
     const long long count = (long long)row_blocks * out_blocks;
-    if (count > 0xffffff00LL / (64 * P::WAVES)) return XNOR_ERR_SHAPE;
+    static_assert(64 * P::WAVES == 512);
+    if (count > W8_MOST_TILES) return XNOR_ERR_SHAPE;
     auto kernel = w8_tiles_kernel<P, ALIGNED, SHARES>;
     if (hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess) return XNOR_ERR_HIP;
     kernel<<<dim3((unsigned)((count + 7) / 8 * 8), (unsigned)shares), dim3(64 * P::WAVES), lds, stream>>>(a, row_blocks, out_blocks);

@@ -60,3 +60,14 @@ def test_sizes_that_the_kernel_of_few_products_cannot_take(lib):
         assert lib.gradient(rows, 1, 100, 0, 0, 0) and lib.gradient(rows, 100, 1, 32, 1, 1)      # (it takes pairs of columns)
     for size in (1, 2 ** 24):
         assert lib.product(65535 * 64, 131071, size) > 0 and lib.gradient(65535 * 64, size, 2 ** 11, 0, 0, 0) >= 0      # (no overflow)
+
+
+def test_the_largest_products_fit_a_launch(lib):
+    """Outputs up to the memory's size (288 GB of 16 bits: 2^37 results and some) never need more tiles than one launch holds: those of 128 give way to those of 256."""
+    most = 0xffffff00 // 512
+    for rows, out in ((65535 * 64, 32768), (65535 * 64, 36000), (2 ** 20, 140000), (2 ** 14, 2 ** 23 + 5), (9000, 2 ** 24)):
+        for cin in (1, 16, 64, 100, 128, 256, 1000, 1024, 9216, 131071):
+            route = lib.product(rows, cin, out)
+            if route >= 1280:
+                side = 256 if route >= 2560 else 128
+                assert -(-rows // side) * -(-out // side) <= most, (rows, cin, out, route)
