@@ -144,7 +144,9 @@ class HiddenAnswer:
 class HiddenTraining:
     """Norm, hidden layer, activation and classifier, trained by plain gradient descent on the mean log probability of one label per row.
 
-    The weights are float32; both products read them, and their rows, in 8 bits, and the backward pass takes these roundings for the identity.
+    The weights are float32; both products read them, and their rows, in 8 bits, and the backward pass takes these roundings for the identity:
+    the gradients of the rows come from the float32 weights that are trained (a code's half step, 1 / 254 of an output's largest, from those
+    that the products read), the gradients of the weights from the 8-bit rows, the only ones that are kept.
     Nothing of the forward pass is kept in more than 8 bits but the logits."""
 
     def __init__(self, norm_weight, hidden, head, rows, function="gelu", gated=False, kept_group=128):
