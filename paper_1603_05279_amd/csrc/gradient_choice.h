@@ -45,8 +45,8 @@ inline GradientChoice gradient_tiles(const GradientParts &p, int in, int out, in
     return middle < small ? GradientChoice{false, 128, middle} : GradientChoice{false, 64, small};
 }
 
-// The direct kernel by its time in us, fitted likewise; the others' range, staging and launches take 13 and their way through memory.  2 rows 371 -> 2011 bfloat16 4.8 and
-// 12, 64 rows 1003 -> 1000 float32 7.4 and 16, 256 rows 1024 -> 1024 bfloat16 10.5 and 16, 777 rows 1003 -> 1000 float32 25 and 28; 2048 rows 512 -> 512 bfloat16 52 and 25, 64 rows
+// The direct kernel by its time in us, fitted likewise; the others' range, staging and launches take 13 and their way through memory.  2 rows 371 -> 2011 bfloat16 4.5 and
+// 12, 64 rows 1003 -> 1000 float32 6.4 and 15, 256 rows 1024 -> 1024 bfloat16 11 and 17, 777 rows 1003 -> 1000 float32 25 and 27; 2048 rows 512 -> 512 bfloat16 52 and 23, 64 rows
 // 4096 -> 4096 84 and 25.  Over 70 products (1 to 1156 rows, 17 to 2900 inputs and outputs) the choice takes 1.001 of the faster one's time.
 inline bool gradient_direct_is_faster(const GradientParts &p, int rows, int in, int out, const GradientChoice &staged)
 {

@@ -88,8 +88,9 @@ template <int F> struct Point {
             value = x > 0.0f ? x : x != x ? x : 0.0f;
             slope = x > 0.0f ? 1.0f : x != x ? x : 0.0f;
         } else if (F == XNOR_GELU) {
-            // Phi(-|x|) = erfc(z) / 2 with z = |x| / sqrt 2;  erfc(z) e^(z^2) / t is a polynomial of t = 1 / (1 + z / 2) to 5e-8 of it (fitted to its values in 64 bits, 3e-7
-            // with float32's roundings; erfcf takes three times as long)
+            // Phi(-|x|) = erfc(z) / 2 with z = |x| / sqrt 2;  erfc(z) e^(z^2) / t is nearly a polynomial of t = 1 / (1 + z / 2) (the substitution of Press et al., Numerical
+            // Recipes, sec. 6.2).  These coefficients are a fit to its values in 64 bits, made here, and are within 8.4e-8 of it up to |x| = 14.5, where the results end; what
+            // comes out is within 5.2e-7 of GELU(x) down to x = -12.  (erfcf takes three times as long.)
             const float a = near_zero(x), square = a * a, root = root_exp_minus(0.5f * square, 0.5f * __builtin_fmaf(a, a, -square));
             const float t = reciprocal(__builtin_fmaf(a, 0.353553391f, 1.0f));
             constexpr float c[9] = {0.2820855975f, 0.2823898494f, 0.2429982424f, 0.2031030208f, -0.02760601416f, 0.2794856131f, -0.4884357750f, 0.2851699591f, -0.05919053033f};
@@ -201,8 +202,8 @@ template <int TYPE, int F, bool GATED> struct Act8 {
 };
 
 // The same rows through f.  kept only where the halves of a gated row are whole groups (and eights) of columns: otherwise q8_rows_kernel writes it.
-// What bounds it: the memory (2048 x 4096 bfloat16, values and kept: SiLU of gated rows 18.1 us, 3.7 TB/s; ReLU of 2048 x 9216 22.5 us, 4.2 TB/s); GELU the vector unit
-// (15.9 us, 2.6 TB/s: 19.5 us with erfcf and expf).  Gated rows whose halves are not whole groups go through both kernels: 25.7 us for 2048 x 4100.
+// What bounds it: the vector unit, and the memory behind it: 2048 x 4096 bfloat16, values and kept: GELU 16 us, of which vector instructions take 13 (19.5 us with erfcf and
+// expf); SiLU of gated rows 19 us, 15 of them (67 MB at the copy's rate 13.5).  ReLU of 2048 x 9216 waits for the memory: 21.5 us, 94 MB at 4.4 TB/s.  Gated rows whose halves are not whole groups go through both kernels: 25.7 us for 2048 x 4100.
 template <int TYPE, int F, bool GATED, int STEPS> __global__ __launch_bounds__(1024) void activation_kernel(RowArgs a)
 {
     typedef real_t<TYPE> T;
@@ -306,7 +307,8 @@ __device__ __forceinline__ void kept_8(const int8_t *p, int n, float *v)
 }
 
 // Eight columns per thread, blockDim.y rows per workgroup, so that rows and columns take no division per thread and scales none per value (both together 23.8 us instead of
-// 19.4 below).  What bounds it: the memory (2048 x 4096 bfloat16, SiLU of gated rows 19.4 us, 3.5 TB/s; GELU 14.7 us, 2.9 TB/s; ReLU of 2048 x 9216 20.1 us, 4.7 TB/s).
+// 19.4 below).  What bounds it: 2048 x 4096 bfloat16, GELU 15.5 us, of which vector instructions take 11 (42 MB at the copy's rate 8.5); SiLU of gated rows 19.5 us, 67 MB
+// (13.5) beside 10 of vector instructions, four streams of rows at once; ReLU of 2048 x 9216 the memory, 17 to 20 us, 4.7 TB/s and more.
 template <int TYPE, int F, bool GATED> __global__ __launch_bounds__(256) void activation_grad_kernel(BackwardArgs a)
 {
     typedef real_t<TYPE> T;

@@ -8,7 +8,7 @@
 //   product the sums, and the powers of two taken out again
 // Few products go through none of it: gradient_direct_kernel below.
 // With one scale per row the scale goes to g instead, sum_r (g[r][o] scale[r]) q[r][k], and q is an operand as it is: float32 gradients and weights then take two products of
-// parts and not three (2048 rows 4096 -> 8192 485 and 279 us).
+// parts and not three (2048 rows 4096 -> 8192 472 and 277 us).
 #include "xnor_internal.h"
 #include "gradient_choice.h"
 #include "lowbit.h"
@@ -205,7 +205,8 @@ template <int TYPE> __global__ __launch_bounds__(256) void gradient_stage_kernel
         }
     }
     __syncthreads();
-    // eight lanes write the 64 rows of a column
+    // eight lanes write the 64 rows of a column.  (One unit at a time: side by side, which is no faster, the last stores end the program without an instruction behind them, and a
+    // reader of the listing takes the next program's first ones for what overwrites their registers.)
     const int parts = is_g ? p.parts_g : p.parts_x;
     uint8_t *to = a.work + (is_g ? p.g_at : p.x_at);
 #pragma unroll 1
@@ -243,8 +244,8 @@ __device__ __forceinline__ void add_results(const GradArgs &a, size_t at, f32x4 
 constexpr int TURNED = 32 * (64 * 4 + 16);          // bytes of 32 outputs x 64 inputs, outputs 16 bytes further apart
 template <class P> constexpr int lds_bytes() { return std::max(P::BUFFERS * P::BYTES, P::WAVES * TURNED); }
 
-// What bounds it: 2048 rows 4096 -> 8192, bfloat16 throughout, 125 us of 164 (a library's product of bfloat16 matrices of these sizes 116): matrix instructions and the loads of
-// their operands, which overlap in part; the others are the range (16) and the staging (22, 88 MB, 4 TB/s).  256 rows 9216 -> 4096 to float32 58 us: 32 with
+// What bounds it: 2048 rows 4096 -> 8192, bfloat16 throughout, 134 to 140 us by itself (a library's product of bfloat16 matrices of these sizes 116): matrix instructions and the
+// loads of their operands, which overlap in part; the range takes 17 and the staging 28 (88 MB), all three one behind the other 164 to 176.  256 rows 9216 -> 4096 to float32 58 us: 32 with
 // the first chunk alone (151 MB of results), 4 more for each of the other seven (57 MB out of L2), which the results hardly hide (tiles of 256 x 128, more of them in LDS or on a CU,
 // waves of two priorities, stores past the caches or without turning: 3 us at most).
 template <class P> __global__ __launch_bounds__(64 * P::WAVES) void gradient_product_kernel(GradArgs a, int blocks_x, int blocks_g)
@@ -296,7 +297,7 @@ template <class P> __global__ __launch_bounds__(64 * P::WAVES) void gradient_pro
 
 // Few products: one launch, 64 outputs x 64 inputs to a workgroup, in float32 throughout.  The matrix instructions of two rows take their operands as they lie: a lane's are one row's,
 // neighbouring lanes' neighbouring columns (two of them each, for two tiles).  Eight waves share the rows, two at a time, and their sums meet in LDS.
-// What bounds it: launch, first loads and last sums up to 100 rows (7.4 us), behind them 0.022 us a row for up to 256 workgroups, 1.6 times what the matrix instructions take
+// What bounds it: launch, first loads and last sums up to 64 rows (6.4 us), behind them 0.022 us a row for up to 256 workgroups, 1.6 times what the matrix instructions take
 // at 2.4 GHz (addresses by steps in place of products, more rows ahead: no change).
 constexpr int DIRECT_WAVES = 8;
 struct DirectShared {
